@@ -374,6 +374,115 @@ gnmr_status gnmr_actuator_info(const gnmr_actuator* act, int64_t* rows, int64_t*
 
 gnmr_status gnmr_actuator_destroy(gnmr_actuator* act);
 
+/* ---------------------------------------------------------------------------
+ * The operators of a mixture-of-experts training step under the controller:
+ * products grouped by expert, the INT8 low-cost path as an 8-bit product, and
+ * the orthogonalised update.  All are asynchronous on `stream`, allocate
+ * nothing, keep nothing between calls and can be captured in a HIP graph;
+ * GNMR_E_INVALID (nothing launched) on a bad argument, GNMR_E_HIP on a launch
+ * failure.  No output may overlap an input or another output: strided matrices
+ * count from their first element to their last (checked).
+ * ------------------------------------------------------------------------- */
+
+/* Which rows (tokens) of an activation matrix belong to which group (expert).
+ * Rows lie sorted by group: group e has rows [offsets[e], offsets[e + 1]), and
+ * may have none.  offsets is device memory, read when the kernels run (a router
+ * on the device can have written it): non-decreasing, offsets[0] = 0, none above
+ * rows.  Other values are clamped to that, so that no access leaves a buffer;
+ * which rows then belong to whom is undefined.  Rows from offsets[num_groups] on belong to
+ * no group (room in a buffer of fixed size); the grouped products set theirs to 0.
+ *
+ * With d_mask (device bytes, e.g. the controller's mask when the experts are its
+ * units), only groups e with (d_mask[e] != 0) == mask_value are computed; the
+ * outputs of the others stay untouched.  Two calls with mask_value 1 and 0 so send
+ * each expert down its recovery or its low-cost path without the host knowing A_t. */
+typedef struct {
+  const int32_t* offsets;  /* device [num_groups + 1], or NULL: one group has all rows */
+  const uint8_t* d_mask;   /* device [num_groups], or NULL: every group             */
+  int64_t rows;            /* rows of the matrices, 0 .. 2^31 - 257                  */
+  int32_t num_groups;      /* 1 .. 65536                                             */
+  int32_t mask_value;      /* 0 or 1                                                 */
+} gnmr_groups;
+
+/* Products of an expert layer with weights w: device bf16
+ * [num_groups][out_features][in_features], contiguous.
+ *   gnmr_grouped_linear:  y[t][o]  = bf16_rne( sum_i x[t][i]  w_e[o][i] )
+ *   gnmr_grouped_dgrad:   dx[t][i] = bf16_rne( sum_o dy[t][o] w_e[o][i] )
+ * for every row t of group e (fp32 accumulation).  x, dx: device bf16 [rows][in_features],
+ * dy, y: device bf16 [rows][out_features], rows *_stride elements apart (at least the
+ * features, a multiple of 8, below 2^22).  Features are multiples of 8 below 2^22; all
+ * pointers 16-byte aligned. */
+gnmr_status gnmr_grouped_linear(const gnmr_groups* groups, const void* x, int64_t x_stride,
+                                const void* w, void* y, int64_t y_stride, int32_t out_features,
+                                int32_t in_features, void* stream);
+gnmr_status gnmr_grouped_dgrad(const gnmr_groups* groups, const void* dy, int64_t dy_stride,
+                               const void* w, void* dx, int64_t dx_stride, int32_t out_features,
+                               int32_t in_features, void* stream);
+
+/* Their weight gradients, with the sums of squares that the controller takes:
+ *   dw_e[o][i] = sum over e's rows t of dy[t][o] x[t][i]   (fp32 accumulation)
+ * dw: device [num_groups][out_features][in_features] of dw_dtype, GNMR_BF16 (one rounding)
+ * or GNMR_F32.  accumulate = 1 adds the stored gradient in fp32 before that (micro-batches);
+ * a group without rows then keeps its gradient, and gets 0 with accumulate = 0.  partials:
+ * device float [num_groups * gnmr_grouped_wgrad_num_partials(out, in)], written with the
+ * fp32 sum of dw^2 (the stored values) over each 128 x 128 block of each dw_e (row-major block
+ * order, ragged edge blocks included), in a fixed order: deterministic.  With one unit
+ * per expert that is what gnmr_bind_partials and gnmr_step_from_partials take. */
+int64_t gnmr_grouped_wgrad_num_partials(int32_t out_features, int32_t in_features);
+gnmr_status gnmr_grouped_wgrad(const gnmr_groups* groups, const void* dy, int64_t dy_stride,
+                               const void* x, int64_t x_stride, void* dw, int32_t dw_dtype,
+                               int32_t accumulate, float* partials, int32_t out_features,
+                               int32_t in_features, void* stream);
+
+/* Symmetric INT8 codes of the rows of x (tokens of an activation, or output
+ * channels of a weight), one scale a row:
+ *   amax = max |x[r][i]|, codes[r][i] = rint(x[r][i] * (127 / amax)), scale[r] = amax / 127
+ * in fp32, ties to even: the recipe of GNMR_FMT_INT8 with codes and scale kept apart.
+ * x: device bf16 or fp32 (x_dtype) [rows][cols], rows x_stride elements apart (a multiple
+ * of 8), 16-byte aligned; codes: device int8 [rows][cols], contiguous, 8-byte aligned;
+ * scale: device float [rows].  cols a multiple of 8 below 2^17.  A row whose amax is below 2^-100 counts
+ * as zero; a row with an infinity or a NaN gets codes 0 and the scale NaN. */
+gnmr_status gnmr_quantize_rows(const void* x, int32_t x_dtype, int64_t x_stride, void* codes,
+                               float* scale, int64_t rows, int32_t cols, void* stream);
+
+/* The low-cost path of a linear layer in 8 bits, a scale for each token and channel:
+ *   y[t][o] = bf16_rne( (sum_i q[t][i] codes_e[o][i]) * (s[t] * w_scale_e[o]) )
+ * with q, s the codes and scale of row t of x as gnmr_quantize_rows makes them, and
+ * codes, w_scale the weights': device int8 [num_groups][out_features][in_features],
+ * contiguous, 8-byte aligned, and device float [num_groups][out_features].  The sum is
+ * exact.  x: device bf16 [rows][in_features], rows x_stride elements apart; or, with x_scale
+ * (device float [rows]), int8 codes made before, x_stride bytes apart (one quantisation for
+ * several layers that read the same x).  y as in gnmr_grouped_linear.  in_features a multiple of 8
+ * below 2^17.  workspace: device, 16-byte aligned, of at least
+ * gnmr_quantized_linear_workspace(rows, in_features) bytes; NULL with x_scale. */
+int64_t gnmr_quantized_linear_workspace(int64_t rows, int32_t in_features);
+gnmr_status gnmr_quantized_linear(const gnmr_groups* groups, const void* x, int64_t x_stride,
+                                  const float* x_scale, const void* codes, const float* w_scale,
+                                  void* y, int64_t y_stride, int32_t out_features,
+                                  int32_t in_features, void* workspace, int64_t workspace_bytes,
+                                  void* stream);
+
+/* Newton-Schulz orthogonalisation of `count` updates G of one shape: with X X^T of the
+ * smaller side,
+ *   X = G / (||G||_F + eps);  `steps` times:  A = X X^T,  X = a X + (b A + c A A) X;
+ *   out = bf16_rne( scale * X )
+ * in, out: device [count][rows][cols], contiguous, in of in_dtype (GNMR_BF16 or GNMR_F32), out
+ * bf16.  rows, cols 1 .. 65536 (any parity); the products run on the matrix cores in fp16 with
+ * scaled iterates and fp32 accumulation, which holds them to about 2^-11 relative each.
+ * The coefficients have to keep the singular values below 16.  G = 0 gives 0; a G with an
+ * infinity or a NaN gives NaN throughout.  workspace: device, 256-byte aligned, of at least
+ * gnmr_orthogonalize_workspace(rows, cols, count) bytes. */
+typedef struct {
+  int32_t steps;           /* 1 .. 100                                              */
+  float a, b, c;           /* finite; 3.4445, -4.7750, 2.0315 are usual             */
+  float eps;               /* >= 0, finite                                          */
+  float scale;             /* finite                                                */
+} gnmr_newton_schulz;
+int64_t gnmr_orthogonalize_workspace(int32_t rows, int32_t cols, int32_t count);
+gnmr_status gnmr_orthogonalize(const void* in, int32_t in_dtype, void* out, int32_t rows,
+                               int32_t cols, int32_t count, const gnmr_newton_schulz* settings,
+                               void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* gnmr_last_error(void);
 

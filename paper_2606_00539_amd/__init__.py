@@ -16,4 +16,7 @@ from .binding import (GNMR_BF16, GNMR_BUDGET_ACTIVE, GNMR_BUDGET_ADMITTED,  # no
                       gnmr_set_profiling, gnmr_set_state, gnmr_state_size, gnmr_step,
                       gnmr_step_from_norms, gnmr_sumsq, gnmr_sumsq_noalloc, gnmr_wgrad_num_tiles,
                       gnmr_wgrad_sumsq, gnmr_wgrad_sumsq_batched, gnmr_bind_partials, gnmr_step_from_partials,
-                      load_library)
+                      gnmr_grouped_dgrad, gnmr_grouped_linear, gnmr_grouped_wgrad,
+                      gnmr_grouped_wgrad_num_partials, gnmr_orthogonalize,
+                      gnmr_orthogonalize_workspace, gnmr_quantize_rows, gnmr_quantized_linear,
+                      gnmr_quantized_linear_workspace, load_library)

@@ -11,10 +11,11 @@ ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libgnmr.so")
 SOURCES = [os.path.join(PKG, "csrc", f)
            for f in ("gnmr_runtime.hip", "k1_sumsq.hip", "k23_control.hip", "k123_step.hip",
-                     "k4_actuator.hip", "k5_wgrad.hip")]
+                     "k4_actuator.hip", "k5_wgrad.hip", "expert_runtime.hip", "k6_grouped.hip",
+                     "k7_quantized.hip", "k8_orthogonal.hip")]
 HEADERS = [os.path.join(PKG, "csrc", f)
-           for f in ("gnmr_internal.h", "k1_geometry.h", "k1_item.h", "k3_pool.h", "lane_ops.h",
-                     "launch_tag.h", "unit_step.h")] + [os.path.join(ROOT, "include", "gnmr.h")]
+           for f in ("gnmr_internal.h", "groups.h", "host_call.h", "k1_geometry.h", "k1_item.h",
+                     "k3_pool.h", "lane_ops.h", "launch_tag.h", "mm_tile.h", "unit_step.h")] + [os.path.join(ROOT, "include", "gnmr.h")]
 
 # Marshalling of the per-step calls (host code), for the Python that builds it: the
 # name carries that Python's ABI, so that no other one loads it.

@@ -34,7 +34,10 @@ EXPORTED = ("gnmr_init", "gnmr_destroy", "gnmr_step", "gnmr_step_from_norms", "g
             "gnmr_last_error", "gnmr_actuator_create", "gnmr_actuate", "gnmr_actuator_info",
             "gnmr_actuator_destroy", "gnmr_wgrad_num_tiles", "gnmr_wgrad_sumsq",
             "gnmr_bind_partials", "gnmr_step_from_partials", "gnmr_wgrad_sumsq_batched",
-            "gnmr_actuate_matrix", "gnmr_sumsq_noalloc")
+            "gnmr_actuate_matrix", "gnmr_sumsq_noalloc", "gnmr_grouped_linear",
+            "gnmr_grouped_dgrad", "gnmr_grouped_wgrad_num_partials", "gnmr_grouped_wgrad",
+            "gnmr_quantize_rows", "gnmr_quantized_linear_workspace", "gnmr_quantized_linear",
+            "gnmr_orthogonalize_workspace", "gnmr_orthogonalize")
 GNMR_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -67,6 +70,17 @@ class gnmr_wgrad_problem(ctypes.Structure):
                 ("tokens", ctypes.c_int64), ("out_features", ctypes.c_int32),
                 ("in_features", ctypes.c_int32), ("accumulate", ctypes.c_int32),
                 ("reserved", ctypes.c_int32)]
+
+
+class gnmr_groups(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("d_mask", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("num_groups", ctypes.c_int32),
+                ("mask_value", ctypes.c_int32)]
+
+
+class gnmr_newton_schulz(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
 class gnmr_stats(ctypes.Structure):
@@ -117,6 +131,12 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
         "gnmr_wgrad_sumsq_batched": [P, I32, P, P],
         "gnmr_step_from_partials": [P, P, D, D, P],
         "gnmr_sumsq_noalloc": [I32, P, P, P],
+        "gnmr_grouped_linear": [P, P, I64, P, P, I64, I32, I32, P],
+        "gnmr_grouped_dgrad": [P, P, I64, P, P, I64, I32, I32, P],
+        "gnmr_grouped_wgrad": [P, P, I64, P, I64, P, I32, I32, P, I32, I32, P],
+        "gnmr_quantize_rows": [P, I32, I64, P, P, I64, I32, P],
+        "gnmr_quantized_linear": [P, P, I64, P, P, P, P, I64, I32, I32, P, I64, P],
+        "gnmr_orthogonalize": [P, I32, P, I32, I32, I32, P, P, I64, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -124,6 +144,12 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
         fn.restype = ctypes.c_int
     lib.gnmr_wgrad_num_tiles.argtypes = [I32, I32]
     lib.gnmr_wgrad_num_tiles.restype = I64
+    lib.gnmr_grouped_wgrad_num_partials.argtypes = [I32, I32]
+    lib.gnmr_grouped_wgrad_num_partials.restype = I64
+    lib.gnmr_quantized_linear_workspace.argtypes = [I64, I32]
+    lib.gnmr_quantized_linear_workspace.restype = I64
+    lib.gnmr_orthogonalize_workspace.argtypes = [I32, I32, I32]
+    lib.gnmr_orthogonalize_workspace.restype = I64
     lib.gnmr_last_error.argtypes = []
     lib.gnmr_last_error.restype = ctypes.c_char_p
     if path == _LIB_PATH:
@@ -403,6 +429,76 @@ def gnmr_actuator_info(act) -> dict:
 
 def gnmr_actuator_destroy(act) -> None:
     _check(load_library().gnmr_actuator_destroy(act))
+
+
+# -- the expert step's operators ----------------------------------------------
+# `offsets` and `mask` are device pointers (ints, tensors or None): group e has rows
+# [offsets[e], offsets[e + 1]), and with a mask only groups whose entry is mask_value count.
+
+def _groups(rows, num_groups, offsets, mask, mask_value):
+    return ctypes.byref(gnmr_groups(None if offsets is None else _dptr(offsets),
+                                    None if mask is None else _dptr(mask), int(rows),
+                                    int(num_groups), int(mask_value)))
+
+
+def gnmr_grouped_linear(x, x_stride, w, y, y_stride, rows, num_groups, out_features, in_features,
+                        offsets=None, mask=None, mask_value=1, stream=None) -> None:
+    _check(load_library().gnmr_grouped_linear(
+        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride), _dptr(w),
+        _dptr(y), int(y_stride), int(out_features), int(in_features), _stream(stream)))
+
+
+def gnmr_grouped_dgrad(dy, dy_stride, w, dx, dx_stride, rows, num_groups, out_features,
+                       in_features, offsets=None, mask=None, mask_value=1, stream=None) -> None:
+    _check(load_library().gnmr_grouped_dgrad(
+        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride), _dptr(w),
+        _dptr(dx), int(dx_stride), int(out_features), int(in_features), _stream(stream)))
+
+
+def gnmr_grouped_wgrad_num_partials(out_features, in_features) -> int:
+    return int(load_library().gnmr_grouped_wgrad_num_partials(int(out_features),
+                                                              int(in_features)))
+
+
+def gnmr_grouped_wgrad(dy, dy_stride, x, x_stride, dw, dw_dtype, accumulate, partials, rows,
+                       num_groups, out_features, in_features, offsets=None, mask=None,
+                       mask_value=1, stream=None) -> None:
+    _check(load_library().gnmr_grouped_wgrad(
+        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride), _dptr(x),
+        int(x_stride), _dptr(dw), int(dw_dtype), int(accumulate), _dptr(partials),
+        int(out_features), int(in_features), _stream(stream)))
+
+
+def gnmr_quantize_rows(x, x_dtype, x_stride, codes, scale, rows, cols, stream=None) -> None:
+    _check(load_library().gnmr_quantize_rows(_dptr(x), int(x_dtype), int(x_stride), _dptr(codes),
+                                             _dptr(scale), int(rows), int(cols), _stream(stream)))
+
+
+def gnmr_quantized_linear_workspace(rows, in_features) -> int:
+    return int(load_library().gnmr_quantized_linear_workspace(int(rows), int(in_features)))
+
+
+def gnmr_quantized_linear(x, x_stride, x_scale, codes, w_scale, y, y_stride, rows, num_groups,
+                          out_features, in_features, workspace=None, workspace_bytes=0,
+                          offsets=None, mask=None, mask_value=1, stream=None) -> None:
+    _check(load_library().gnmr_quantized_linear(
+        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride),
+        None if x_scale is None else _dptr(x_scale), _dptr(codes), _dptr(w_scale), _dptr(y),
+        int(y_stride), int(out_features), int(in_features),
+        None if workspace is None else _dptr(workspace), int(workspace_bytes), _stream(stream)))
+
+
+def gnmr_orthogonalize_workspace(rows, cols, count) -> int:
+    return int(load_library().gnmr_orthogonalize_workspace(int(rows), int(cols), int(count)))
+
+
+def gnmr_orthogonalize(x, x_dtype, out, rows, cols, count, steps, coefficients, eps, scale,
+                       workspace, workspace_bytes, stream=None) -> None:
+    a, b, c = coefficients
+    z = gnmr_newton_schulz(int(steps), float(a), float(b), float(c), float(eps), float(scale))
+    _check(load_library().gnmr_orthogonalize(
+        _dptr(x), int(x_dtype), _dptr(out), int(rows), int(cols), int(count), ctypes.byref(z),
+        None if workspace is None else _dptr(workspace), int(workspace_bytes), _stream(stream)))
 
 
 class Actuator:

@@ -153,4 +153,81 @@ bool single_launch_update_select(const UpdateArgs& a, int64_t num_items);
 hipError_t launch_update_select(const UpdateArgs& u, const SelectArgs& s, int64_t num_items,
                                 hipStream_t st);
 
+// Which rows of an activation matrix belong to which group (expert): group e has
+// rows [offsets[e], offsets[e+1]), offsets[0] counting as 0; without offsets one group has
+// them all.  Groups whose mask entry is not mask_value are left out.
+struct GroupArgs {
+  const int32_t* offsets;  // device [num + 1] or nullptr
+  const uint8_t* mask;     // device [num] or nullptr
+  int32_t num;
+  int32_t mask_value;      // 0 or 1
+  int32_t rows;
+};
+
+// K6 (grouped products; see k6_grouped.hip)
+constexpr int kGroupedBlock = 128;  // edge of the blocks of one sum of squares
+struct GroupedRows {
+  GroupArgs g;
+  const uint16_t* in;   // [rows][K], in_stride elements apart
+  const uint16_t* w;    // linear: [num][N][K], dgrad: [num][K][N]
+  uint16_t* out;        // [rows][N], out_stride elements apart
+  int64_t in_stride, out_stride;
+  int32_t N, K, tiles_n;
+};
+struct GroupedWgrad {
+  GroupArgs g;
+  const uint16_t* dy;   // [rows][M], dy_stride elements apart
+  const uint16_t* x;    // [rows][N], x_stride elements apart
+  void* dw;             // [num][M][N]
+  float* partials;      // [num][blocks of kGroupedBlock, row-major]
+  int64_t dy_stride, x_stride;
+  int32_t M, N, tiles_m, tiles_n;
+};
+// Workgroups that the largest launch of such a call can need.
+int64_t grouped_rows_workgroups(const GroupedRows& a);
+hipError_t launch_grouped_rows(const GroupedRows& a, bool dgrad, hipStream_t s);
+hipError_t launch_grouped_wgrad(const GroupedWgrad& a, bool f32, bool accumulate, hipStream_t s);
+
+// K7 (INT8 linear; see k7_quantized.hip)
+struct QuantizeRows {
+  const void* x;          // [rows][cols] bf16 or fp32, x_stride elements apart
+  int8_t* codes;          // [rows][cols], codes_stride bytes apart
+  float* scale;           // [rows]
+  int64_t x_stride, codes_stride;
+  int32_t rows, cols;
+};
+struct QuantizedLinear {
+  GroupArgs g;
+  const int8_t* q;        // [rows][K], q_stride bytes apart
+  const float* q_scale;   // [rows]
+  const int8_t* w;        // [num][N][K]
+  const float* w_scale;   // [num][N]
+  uint16_t* y;            // [rows][N], y_stride elements apart
+  int64_t q_stride, y_stride;
+  int32_t N, K, tiles_n;
+};
+int64_t quantized_codes_stride(int32_t in_features);
+int64_t quantized_linear_workgroups(const GroupArgs& g, int32_t out_features);
+hipError_t launch_quantize_rows(const QuantizeRows& a, bool f32, hipStream_t s);
+hipError_t launch_quantized_linear(QuantizedLinear a, hipStream_t s);
+
+// K8 (orthogonalisation; see k8_orthogonal.hip)
+struct Orthogonal {
+  const void* in;         // [count][rows][cols] bf16 or fp32
+  __bf16* out;            // [count][rows][cols]
+  int32_t rows, cols, count;
+  float ca, cb, cc, eps, scale;
+  bool f32;
+  // set by launch_orthogonal
+  bool flip, first;       // flip: X is the transpose of the update
+  int32_t m, n, mp, np, now, tiles_m, tiles_n;
+  double* sums;           // [count][partial sums of squares]
+  float* factor;          // [count], first iteration: X = factor * what is held
+  _Float16* x[2];         // [count][mp][np]
+  _Float16 *A, *B;        // [count][mp][mp]
+};
+int64_t orthogonal_workgroups(const Orthogonal& a);
+int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count);
+hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream_t s);
+
 }  // namespace gnmr

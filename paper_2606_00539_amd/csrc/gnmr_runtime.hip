@@ -11,24 +11,17 @@
 #include <vector>
 
 #include "gnmr_internal.h"
+#include "host_call.h"
 
+using gnmr::fail;
+using gnmr::intersect;
 using gnmr::Item;
+using gnmr::Span;
+using gnmr::span_of;
 
 namespace {
 
 thread_local std::string g_last_error;
-
-gnmr_status fail(gnmr_status st, const std::string& msg) {
-  g_last_error = msg;
-  return st;
-}
-
-#define GNMR_HIP(expr)                                                                 \
-  do {                                                                                 \
-    hipError_t e_ = (expr);                                                            \
-    if (e_ != hipSuccess)                                                              \
-      return fail(GNMR_E_HIP, std::string(#expr) + ": " + hipGetErrorString(e_));      \
-  } while (0)
 
 constexpr uint32_t kStateMagic = 0x524D4E47u;  // "GNMR"
 constexpr uint32_t kStateVersion = 4;
@@ -66,21 +59,6 @@ struct DeviceGuard {
     if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
   }
 };
-
-// A byte range [lo, hi) of device memory that buffer `id` covers.
-struct Span {
-  uintptr_t lo, hi;
-  int64_t id;
-};
-
-Span span_of(const void* p, int64_t bytes, int64_t id) {
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return Span{lo, lo + uintptr_t(bytes), id};
-}
-
-bool intersect(const Span& a, const Span& b) {
-  return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
-}
 
 // Index of a write that overlaps another write, or a read of a different id;
 // -1 when there is none.  O((W + R) log R): reads sorted by start, with the
@@ -130,6 +108,11 @@ int64_t find_overlap(std::vector<Span> w, std::vector<Span> r) {
 }
 
 }  // namespace
+
+gnmr_status gnmr::fail(gnmr_status st, const std::string& msg) {
+  g_last_error = msg;
+  return st;
+}
 
 struct gnmr_ctx {
   int device = 0;
