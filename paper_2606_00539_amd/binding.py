@@ -164,19 +164,34 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
 _PER_STEP = ("gnmr_step", "gnmr_step_from_norms", "gnmr_step_from_partials", "gnmr_sumsq",
              "gnmr_actuate", "gnmr_actuate_matrix", "gnmr_wgrad_sumsq",
              "gnmr_wgrad_sumsq_batched")
+_EXPERT_STEP = ("gnmr_grouped_linear", "gnmr_grouped_dgrad", "gnmr_grouped_wgrad",
+                "gnmr_quantize_rows", "gnmr_quantized_linear", "gnmr_orthogonalize")
+
+
+def _addresses(lib, names):
+    return {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names}
+
+
+def _none_or(p):
+    return None if p is None else _dptr(p)
+
+
+def _groups(rows, num_groups, offsets, mask, mask_value):
+    return ctypes.byref(gnmr_groups(_none_or(offsets), _none_or(mask), int(rows), int(num_groups),
+                                    int(mask_value)))
 
 
 class _CtypesCalls:
     """The functions of the module _calls by ctypes."""
 
     def __init__(self, lib):
-        self.bind(lib, {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value
-                        for n in _PER_STEP})
+        self._f = {}
+        self.bind(lib, _addresses(lib, _PER_STEP + _EXPERT_STEP))
 
     def bind(self, lib, addresses):
         """Calls what is at `addresses`, with the argument types of lib's functions."""
-        self._f = {n: ctypes.CFUNCTYPE(ctypes.c_int, *getattr(lib, n).argtypes)(a)
-                   for n, a in addresses.items()}
+        self._f.update({n: ctypes.CFUNCTYPE(ctypes.c_int, *getattr(lib, n).argtypes)(a)
+                        for n, a in addresses.items()})
 
     def step(self, ctx, alpha_t, beta_t, seg_ptr, stream):
         ptrs = None if seg_ptr is None else _ptr_array(seg_ptr)
@@ -218,6 +233,48 @@ class _CtypesCalls:
         return self._f["gnmr_wgrad_sumsq_batched"](arr, len(ps), _dptr(tile_sumsq),
                                                    _stream(stream))
 
+    def grouped_linear(self, rows, num_groups, offsets, mask, mask_value, x, x_stride, w, y,
+                       y_stride, out_features, in_features, stream):
+        return self._f["gnmr_grouped_linear"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride),
+            _dptr(w), _dptr(y), int(y_stride), int(out_features), int(in_features),
+            _stream(stream))
+
+    def grouped_dgrad(self, rows, num_groups, offsets, mask, mask_value, dy, dy_stride, w, dx,
+                      dx_stride, out_features, in_features, stream):
+        return self._f["gnmr_grouped_dgrad"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride),
+            _dptr(w), _dptr(dx), int(dx_stride), int(out_features), int(in_features),
+            _stream(stream))
+
+    def grouped_wgrad(self, rows, num_groups, offsets, mask, mask_value, dy, dy_stride, x,
+                      x_stride, dw, dw_dtype, accumulate, partials, out_features, in_features,
+                      stream):
+        return self._f["gnmr_grouped_wgrad"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride),
+            _dptr(x), int(x_stride), _dptr(dw), int(dw_dtype), int(accumulate), _dptr(partials),
+            int(out_features), int(in_features), _stream(stream))
+
+    def quantize_rows(self, x, x_dtype, x_stride, codes, scale, rows, cols, stream):
+        return self._f["gnmr_quantize_rows"](_dptr(x), int(x_dtype), int(x_stride), _dptr(codes),
+                                             _dptr(scale), int(rows), int(cols), _stream(stream))
+
+    def quantized_linear(self, rows, num_groups, offsets, mask, mask_value, x, x_stride, x_scale,
+                         codes, w_scale, y, y_stride, out_features, in_features, workspace,
+                         workspace_bytes, stream):
+        return self._f["gnmr_quantized_linear"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride),
+            _none_or(x_scale), _dptr(codes), _dptr(w_scale), _dptr(y), int(y_stride),
+            int(out_features), int(in_features), _none_or(workspace), int(workspace_bytes),
+            _stream(stream))
+
+    def orthogonalize(self, x, x_dtype, out, rows, cols, count, steps, a, b, c, eps, scale,
+                      workspace, workspace_bytes, stream):
+        z = gnmr_newton_schulz(int(steps), float(a), float(b), float(c), float(eps), float(scale))
+        return self._f["gnmr_orthogonalize"](
+            _dptr(x), int(x_dtype), _dptr(out), int(rows), int(cols), int(count),
+            ctypes.byref(z), _none_or(workspace), int(workspace_bytes), _stream(stream))
+
 
 def _load_calls(lib):
     """The module of the per-step calls, set to the functions of `lib`."""
@@ -227,7 +284,8 @@ def _load_calls(lib):
         warnings.warn("the module _calls is not built for this Python (__graft_entry__.build() "
                       "does it): the per-step calls take longer through ctypes", RuntimeWarning)
         return _CtypesCalls(lib)
-    calls.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _PER_STEP})
+    calls.bind(_addresses(lib, _PER_STEP))
+    calls.bind_experts(_addresses(lib, _EXPERT_STEP))
     return calls
 
 
@@ -435,24 +493,16 @@ def gnmr_actuator_destroy(act) -> None:
 # `offsets` and `mask` are device pointers (ints, tensors or None): group e has rows
 # [offsets[e], offsets[e + 1]), and with a mask only groups whose entry is mask_value count.
 
-def _groups(rows, num_groups, offsets, mask, mask_value):
-    return ctypes.byref(gnmr_groups(None if offsets is None else _dptr(offsets),
-                                    None if mask is None else _dptr(mask), int(rows),
-                                    int(num_groups), int(mask_value)))
-
-
 def gnmr_grouped_linear(x, x_stride, w, y, y_stride, rows, num_groups, out_features, in_features,
                         offsets=None, mask=None, mask_value=1, stream=None) -> None:
-    _check(load_library().gnmr_grouped_linear(
-        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride), _dptr(w),
-        _dptr(y), int(y_stride), int(out_features), int(in_features), _stream(stream)))
+    _check(_native().grouped_linear(rows, num_groups, offsets, mask, mask_value, x, x_stride, w,
+                                    y, y_stride, out_features, in_features, stream))
 
 
 def gnmr_grouped_dgrad(dy, dy_stride, w, dx, dx_stride, rows, num_groups, out_features,
                        in_features, offsets=None, mask=None, mask_value=1, stream=None) -> None:
-    _check(load_library().gnmr_grouped_dgrad(
-        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride), _dptr(w),
-        _dptr(dx), int(dx_stride), int(out_features), int(in_features), _stream(stream)))
+    _check(_native().grouped_dgrad(rows, num_groups, offsets, mask, mask_value, dy, dy_stride, w,
+                                   dx, dx_stride, out_features, in_features, stream))
 
 
 def gnmr_grouped_wgrad_num_partials(out_features, in_features) -> int:
@@ -463,15 +513,13 @@ def gnmr_grouped_wgrad_num_partials(out_features, in_features) -> int:
 def gnmr_grouped_wgrad(dy, dy_stride, x, x_stride, dw, dw_dtype, accumulate, partials, rows,
                        num_groups, out_features, in_features, offsets=None, mask=None,
                        mask_value=1, stream=None) -> None:
-    _check(load_library().gnmr_grouped_wgrad(
-        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride), _dptr(x),
-        int(x_stride), _dptr(dw), int(dw_dtype), int(accumulate), _dptr(partials),
-        int(out_features), int(in_features), _stream(stream)))
+    _check(_native().grouped_wgrad(rows, num_groups, offsets, mask, mask_value, dy, dy_stride, x,
+                                   x_stride, dw, dw_dtype, accumulate, partials, out_features,
+                                   in_features, stream))
 
 
 def gnmr_quantize_rows(x, x_dtype, x_stride, codes, scale, rows, cols, stream=None) -> None:
-    _check(load_library().gnmr_quantize_rows(_dptr(x), int(x_dtype), int(x_stride), _dptr(codes),
-                                             _dptr(scale), int(rows), int(cols), _stream(stream)))
+    _check(_native().quantize_rows(x, x_dtype, x_stride, codes, scale, rows, cols, stream))
 
 
 def gnmr_quantized_linear_workspace(rows, in_features) -> int:
@@ -481,11 +529,9 @@ def gnmr_quantized_linear_workspace(rows, in_features) -> int:
 def gnmr_quantized_linear(x, x_stride, x_scale, codes, w_scale, y, y_stride, rows, num_groups,
                           out_features, in_features, workspace=None, workspace_bytes=0,
                           offsets=None, mask=None, mask_value=1, stream=None) -> None:
-    _check(load_library().gnmr_quantized_linear(
-        _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride),
-        None if x_scale is None else _dptr(x_scale), _dptr(codes), _dptr(w_scale), _dptr(y),
-        int(y_stride), int(out_features), int(in_features),
-        None if workspace is None else _dptr(workspace), int(workspace_bytes), _stream(stream)))
+    _check(_native().quantized_linear(rows, num_groups, offsets, mask, mask_value, x, x_stride,
+                                      x_scale, codes, w_scale, y, y_stride, out_features,
+                                      in_features, workspace, workspace_bytes, stream))
 
 
 def gnmr_orthogonalize_workspace(rows, cols, count) -> int:
@@ -495,10 +541,8 @@ def gnmr_orthogonalize_workspace(rows, cols, count) -> int:
 def gnmr_orthogonalize(x, x_dtype, out, rows, cols, count, steps, coefficients, eps, scale,
                        workspace, workspace_bytes, stream=None) -> None:
     a, b, c = coefficients
-    z = gnmr_newton_schulz(int(steps), float(a), float(b), float(c), float(eps), float(scale))
-    _check(load_library().gnmr_orthogonalize(
-        _dptr(x), int(x_dtype), _dptr(out), int(rows), int(cols), int(count), ctypes.byref(z),
-        None if workspace is None else _dptr(workspace), int(workspace_bytes), _stream(stream)))
+    _check(_native().orthogonalize(x, x_dtype, out, rows, cols, count, steps, a, b, c, eps, scale,
+                                   workspace, workspace_bytes, stream))
 
 
 class Actuator:

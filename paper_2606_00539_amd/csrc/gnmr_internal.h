@@ -220,8 +220,9 @@ struct Orthogonal {
   bool f32;
   // set by launch_orthogonal
   bool flip, first;       // flip: X is the transpose of the update
-  int32_t m, n, mp, np, now, tiles_m, tiles_n;
-  double* sums;           // [count][partial sums of squares]
+  int32_t m, n, mp, np, now, tiles_m, tiles_n, tiles, first_tile, num_tiles;
+  int32_t parts;
+  double* sums;           // [count][parts], partial sums of squares
   float* factor;          // [count], first iteration: X = factor * what is held
   _Float16* x[2];         // [count][mp][np]
   _Float16 *A, *B;        // [count][mp][mp]

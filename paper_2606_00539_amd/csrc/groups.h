@@ -4,6 +4,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -44,6 +45,15 @@ __device__ __forceinline__ void walk(int v, int tiles_m, int tiles_n, int* tm, i
   const int rows = min(tiles_m - first, kRows), at = v % per;
   *tm = first + at % rows;
   *tn = at / rows;
+}
+
+// Position v of the tiles on and above the diagonal of a square of tiles, by columns.
+__device__ __forceinline__ void walk_triangle(int v, int* tm, int* tn) {
+  int c = int((sqrtf(8.0f * float(v) + 1.0f) - 1.0f) * 0.5f);
+  if (c * (c + 1) / 2 > v) --c;  // the root is rounded
+  if ((c + 1) * (c + 2) / 2 <= v) ++c;
+  *tn = c;
+  *tm = v - c * (c + 1) / 2;
 }
 
 struct RowTile {
@@ -104,6 +114,28 @@ __device__ __forceinline__ bool find_row_tile(const GroupArgs& g, int tiles_n, i
     before += int(lane_of(uint32_t(upto), 63));
   }
   return false;
+}
+
+// Microseconds that tiles of 256 x 256 (one workgroup per CU) or 128 x 128 (two per CU) take,
+// `steps` K steps of 128 bytes each, with the whole chip at work.  A 256 tile does twice as much
+// per byte that passes the L1 (the 128 tile's bound: its 32 KiB a step take as long as its
+// matrix-core work), but there are a quarter as many.  Measured a step and beside them: 1.45 and
+// 9 us; 1.05 (two at once; 0.6 alone on a CU) and 8 us.
+inline double us_of_256(double tiles, double steps) {
+  return ceil(tiles / 256.0) * (1.45 * steps + 9.0);
+}
+inline double us_of_128(double tiles, double steps) {
+  const double rest = tiles - 512.0 * floor(tiles / 512.0);
+  return floor(tiles / 512.0) * (1.05 * steps + 8.0) +
+         (rest <= 0.0 ? 0.0 : (rest <= 256.0 ? 0.6 : 1.05) * steps + 8.0);
+}
+
+// Whether a grouped product over `rows` rows and N columns runs in 256 tiles.  The groups' sizes
+// are not known here: each is taken to leave half a tile empty.
+inline bool grouped_in_256(const GroupArgs& g, int N, double steps) {
+  const double empty = g.offsets == nullptr ? 0.0 : 0.5 * std::min<double>(g.num, g.rows);
+  auto tiles = [&](double t) { return ceil(g.rows / t + empty) * ceil(N / t); };
+  return us_of_256(tiles(256.0), steps) < us_of_128(tiles(128.0), steps);
 }
 
 // Tiles of kT rows that `rows` rows in g.num groups (and the rest) can make at most.

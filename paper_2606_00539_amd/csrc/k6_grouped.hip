@@ -19,11 +19,11 @@ namespace gnmr {
 namespace {
 
 using mm::Bf16;
+using mm::f32x4;
 using mm::u32x2;
 using mm::u32x4;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
@@ -32,13 +32,14 @@ __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 1
 __device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 
 // linear (kDgrad false) and dgrad: out[t][n] = sum_k in[t][k] * W_e(n, k).
-template <bool kDgrad, int kTM, int kTN, int kWM, int kStages, int kPerCu>
+template <bool kDgrad, int kT, int kPerCu>
 __global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_rows(const GroupedRows a) {
-  using T = mm::Tile<Bf16, false, kDgrad, kTM, kTN, kWM, kStages>;
+  using D = mm::Depth<false, kDgrad>;
+  using T = mm::Tile<Bf16, false, kDgrad, kT, kT, 2, D::kStep, D::kStages>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
-  if (!find_row_tile<kTM>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
-  const int n0 = t.tn * kTN;
+  if (!find_row_tile<kT>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  const int n0 = t.tn * kT;
   typename T::Acc acc[T::kBM][T::kBN];
   typename T::OpM om;
   typename T::OpN on;
@@ -47,18 +48,31 @@ __global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_rows(const GroupedRow
   on.at(kDgrad ? w + n0 : w + int64_t(n0) * a.K, int64_t(kDgrad ? a.N : a.K) * 2, a.N - n0, wave,
         lane);
   T::product(acc, om, on, t.group < a.g.num ? a.K : 0, wave, lane);
-  T::each(wave, lane, [&](int i, int j, int g, int m, int n) {
-    if (m < t.rows && n0 + n < a.N) {
-      const auto& c = acc[i][j];
-      *reinterpret_cast<u32x2*>(a.out + int64_t(t.row + m) * a.out_stride + n0 + n) =
-          u32x2{pack(c[4 * g], c[4 * g + 1]), pack(c[4 * g + 2], c[4 * g + 3])};
-    }
-  });
+  T::out16(
+      acc, wave, lane,
+      [](int, int, float a0, float a1, float a2, float a3) {
+        return u32x2{pack(a0, a1), pack(a2, a3)};
+      },
+      [&](int m, int n, const u32x4& v) {
+        if (m < t.rows && n0 + n < a.N)
+          *reinterpret_cast<u32x4*>(a.out + int64_t(t.row + m) * a.out_stride + n0 + n) = v;
+      });
 }
 
-template <bool kF32, bool kAcc, int kT, int kStages, int kPerCu>
-__global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_wgrad(const GroupedWgrad a) {
-  using T = mm::Tile<Bf16, true, true, kT, kT, 2, kStages>;
+// The 128 tile's three stages leave room for three workgroups on a CU; where it holds fp32 values
+// to add to, their registers allow two, and there is room for four stages.  64 experts 2048 x
+// 1408, 24,576 rows, three and two on a CU: bf16 269 and 289 us, accumulating 319 and 347, fp32
+// 334 and 365, accumulating 536 and 431.
+template <bool kF32, bool kAcc, int kT>
+struct WgradTile {
+  static constexpr int kPerCu = kT == 256 ? 1 : kF32 && kAcc ? 2 : 3;
+  using T = mm::Tile<Bf16, true, true, kT, kT, 2, 64, kPerCu == 3 ? 3 : 4>;
+};
+
+template <bool kF32, bool kAcc, int kT>
+__global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) void k6_wgrad(
+    const GroupedWgrad a) {
+  using T = typename WgradTile<kF32, kAcc, kT>::T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per = a.tiles_m * a.tiles_n, v = xcd_order(blockIdx.x, a.g.num * per);
   const int e = v / per;
@@ -72,42 +86,65 @@ __global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_wgrad(const GroupedWg
   typename T::OpN on;
   om.at(a.dy + int64_t(begin) * a.dy_stride + m0, a.dy_stride * 2, a.M - m0, wave, lane);
   on.at(a.x + int64_t(begin) * a.x_stride + n0, a.x_stride * 2, a.N - n0, wave, lane);
+  const int64_t base = (int64_t(e) * a.M + m0) * a.N + n0;
+  // Accumulating in 128 tiles, the stored values are on their way while the product runs
+  // (a 256 tile has no registers for them).
+  typedef typename std::conditional<kF32, f32x4, u32x2>::type Old;
+  constexpr bool kEarly = kAcc && kT == 128;
+  Old old[kEarly ? T::kPieces : 1];
+  const int col = T::col(wave, lane);
+  auto there = [&](int row) { return m0 + row < a.M && n0 + col < a.N; };
+  auto stored = [&](int row) {
+    return static_cast<char*>(a.dw) + (base + int64_t(row) * a.N + col) * (kF32 ? 4 : 2);
+  };
+  if constexpr (kEarly) {
+#pragma unroll
+    for (int q = 0; q < T::kPieces; ++q) {
+      const int row = T::row(q, wave, lane);
+      old[q] = there(row) ? *reinterpret_cast<const Old*>(stored(row)) : Old{};
+    }
+  }
   T::product(acc, om, on, end - begin, wave, lane);
   float ss = 0.0f;
-  const int64_t base = int64_t(e) * a.M * a.N;
-  T::each(wave, lane, [&](int i, int j, int g, int m, int n) {
-    if (m0 + m < a.M && n0 + n < a.N) {
-      const auto& c = acc[i][j];
-      const int64_t at = base + int64_t(m0 + m) * a.N + n0 + n;
-      float q[4] = {c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
-      if constexpr (kF32) {
-        f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(a.dw) + at);
-        if constexpr (kAcc) {
-          const f32x4 old = *p;
+  auto square = [&](float q) { ss = fmaf(q, q, ss); };
+  if constexpr (!kF32 && !kAcc) {
+    T::out16(
+        acc, wave, lane,
+        [](int, int, float a0, float a1, float a2, float a3) {
+          return u32x2{pack(a0, a1), pack(a2, a3)};
+        },
+        [&](int m, int n, const u32x4& v) {
+          if (m0 + m < a.M && n0 + n < a.N) {
+            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.dw) + base + int64_t(m) * a.N + n) =
+                v;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) q[k] += old[k];
-        }
-        *p = f32x4{q[0], q[1], q[2], q[3]};
+            for (int k = 0; k < 4; ++k) {
+              square(low(v[k]));
+              square(high(v[k]));
+            }
+          }
+        });
+  } else {
+    T::out32(acc, wave, lane, [&](int q, f32x4 v) {
+      const int row = T::row(q, wave, lane);
+      if (!there(row)) return;
+      Old* p = reinterpret_cast<Old*>(stored(row));
+      Old was{};
+      if constexpr (kEarly) was = old[q];
+      else if constexpr (kAcc) was = *p;
+      if constexpr (kF32) {
+        if constexpr (kAcc) v += was;
+        *p = v;
       } else {
-        u32x2* p = reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.dw) + at);
-        if constexpr (kAcc) {
-          const u32x2 old = *p;
-          q[0] += low(old.x);
-          q[1] += high(old.x);
-          q[2] += low(old.y);
-          q[3] += high(old.y);
-        }
-        const u32x2 r{pack(q[0], q[1]), pack(q[2], q[3])};
+        const u32x2 r{pack(v[0] + low(was.x), v[1] + high(was.x)),
+                      pack(v[2] + low(was.y), v[3] + high(was.y))};
         *p = r;
-        q[0] = low(r.x);
-        q[1] = high(r.x);
-        q[2] = low(r.y);
-        q[3] = high(r.y);
+        v = f32x4{low(r.x), high(r.x), low(r.y), high(r.y)};
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) ss = fmaf(q[k], q[k], ss);
-    }
-  });
+      for (int k = 0; k < 4; ++k) square(v[k]);
+    });
+  }
   ss = wave_sum(ss);
   const int blocks_n = (a.N + kGroupedBlock - 1) / kGroupedBlock;
   const int64_t blocks = int64_t((a.M + kGroupedBlock - 1) / kGroupedBlock) * blocks_n;
@@ -124,22 +161,32 @@ __global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_wgrad(const GroupedWg
   }
 }
 
-template <bool kDgrad, int kTM, int kTN, int kWM, int kStages, int kPerCu>
+template <bool kDgrad, int kT>
 void launch_rows(GroupedRows a, hipStream_t s) {
-  a.tiles_n = (a.N + kTN - 1) / kTN;
-  const int64_t wgs = most_row_tiles(a.g, kTM) * a.tiles_n;
-  hipLaunchKernelGGL((k6_rows<kDgrad, kTM, kTN, kWM, kStages, kPerCu>), dim3(unsigned(wgs)),
-                     dim3(mm::kThreads), 0, s, a);
+  a.tiles_n = (a.N + kT - 1) / kT;
+  hipLaunchKernelGGL((k6_rows<kDgrad, kT, kT == 256 ? 1 : 2>),
+                     dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0, s,
+                     a);
 }
 
 template <bool kF32, bool kAcc>
 void launch_wgrad_of(GroupedWgrad a, hipStream_t s) {
-  constexpr int kT = 128;
-  a.tiles_m = (a.M + kT - 1) / kT;
-  a.tiles_n = (a.N + kT - 1) / kT;
-  hipLaunchKernelGGL((k6_wgrad<kF32, kAcc, kT, 2, 2>),
-                     dim3(unsigned(int64_t(a.g.num) * a.tiles_m * a.tiles_n)), dim3(mm::kThreads),
-                     0, s, a);
+  auto launch = [&](auto edge) {
+    constexpr int kT = decltype(edge)::value;
+    a.tiles_m = (a.M + kT - 1) / kT;
+    a.tiles_n = (a.N + kT - 1) / kT;
+    hipLaunchKernelGGL((k6_wgrad<kF32, kAcc, kT>),
+                       dim3(unsigned(int64_t(a.g.num) * a.tiles_m * a.tiles_n)),
+                       dim3(mm::kThreads), 0, s, a);
+  };
+  // 256 tiles where experts have rows enough to outweigh what a tile takes beside its
+  // steps, and tiles enough for the chip.  us in 128 and 256 tiles, bf16 and accumulating: 64
+  // experts 2048 x 1408 of 384 rows 269 and 282, 319 and 621; 8 of 4096 x 11008 of 1,024
+  // rows 861 and 855, 980 and 1,543; one of 5120 x 13824 of 8,192 rows 1,524 and 951, 1,483 and
+  // 1,096; one of 4096 x 4096 of 4,096 rows 130 and 109, 142 and 133.
+  const int64_t tiles = int64_t(a.g.num) * ((a.M + 255) / 256) * ((a.N + 255) / 256);
+  if (a.g.rows / a.g.num >= 2048 && tiles >= 192) launch(std::integral_constant<int, 256>{});
+  else launch(std::integral_constant<int, 128>{});
 }
 
 }  // namespace
@@ -149,8 +196,11 @@ int64_t grouped_rows_workgroups(const GroupedRows& a) {
 }
 
 hipError_t launch_grouped_rows(const GroupedRows& a, bool dgrad, hipStream_t s) {
-  if (dgrad) launch_rows<true, 128, 128, 2, 2, 2>(a, s);
-  else launch_rows<false, 128, 128, 2, 2, 2>(a, s);
+  const bool large = grouped_in_256(a.g, a.N, (a.K + 63) / 64);
+  if (dgrad && large) launch_rows<true, 256>(a, s);
+  else if (dgrad) launch_rows<true, 128>(a, s);
+  else if (large) launch_rows<false, 256>(a, s);
+  else launch_rows<false, 128>(a, s);
   return hipGetLastError();
 }
 

@@ -14,12 +14,12 @@
 namespace gnmr {
 namespace {
 
+using mm::f32x4;
 using mm::Int8;
 using mm::u32x2;
 using mm::u32x4;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
@@ -102,32 +102,37 @@ __global__ __launch_bounds__(256) void k7_quantize(const QuantizeRows a) {
     *reinterpret_cast<u32x2*>(q + i) = codes(eight<kF32>(x, i), inv);
 }
 
-template <int kTM, int kTN, int kWM, int kStages, int kPerCu>
+template <int kT, int kPerCu>
 __global__ __launch_bounds__(mm::kThreads, kPerCu) void k7_linear(const QuantizedLinear a) {
-  using T = mm::Tile<Int8, false, false, kTM, kTN, kWM, kStages>;
+  using D = mm::Depth<false, false>;
+  using T = mm::Tile<Int8, false, false, kT, kT, 2, D::kStep, D::kStages>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
-  if (!find_row_tile<kTM>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
-  const int n0 = t.tn * kTN, e = t.group < a.g.num ? t.group : 0;
+  if (!find_row_tile<kT>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  const int n0 = t.tn * kT, e = t.group < a.g.num ? t.group : 0;
   typename T::Acc acc[T::kBM][T::kBN];
   typename T::OpM om;
   typename T::OpN on;
   om.at(a.q + int64_t(t.row) * a.q_stride, a.q_stride, t.rows, wave, lane);
   on.at(a.w + (int64_t(e) * a.N + n0) * a.K, a.K, a.N - n0, wave, lane);
   T::product(acc, om, on, t.group < a.g.num ? a.K : 0, wave, lane);
+  const bool none = t.group >= a.g.num;
   const float* sw = a.w_scale + int64_t(e) * a.N + n0;
   const float* sx = a.q_scale + t.row;
-  T::each(wave, lane, [&](int i, int j, int g, int m, int n) {
-    if (m < t.rows && n0 + n < a.N) {
-      float v[4] = {0, 0, 0, 0};
-      if (t.group < a.g.num) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = float(acc[i][j][4 * g + k]) * (sx[m] * sw[n + k]);
-      }
-      *reinterpret_cast<u32x2*>(a.y + int64_t(t.row + m) * a.y_stride + n0 + n) =
-          u32x2{pack(v[0], v[1]), pack(v[2], v[3])};
-    }
-  });
+  T::out16(
+      acc, wave, lane,
+      [&](int m, int n, int a0, int a1, int a2, int a3) {
+        // rows and channels past the last ones read those: nothing of theirs is stored
+        const float s = none ? 0.0f : sx[min(m, t.rows - 1)];
+        const f32x4 w = *reinterpret_cast<const f32x4*>(sw + min(n, a.N - n0 - 4));
+        return none ? u32x2{0, 0}
+                    : u32x2{pack(float(a0) * (s * w[0]), float(a1) * (s * w[1])),
+                            pack(float(a2) * (s * w[2]), float(a3) * (s * w[3]))};
+      },
+      [&](int m, int n, const u32x4& v) {
+        if (m < t.rows && n0 + n < a.N)
+          *reinterpret_cast<u32x4*>(a.y + int64_t(t.row + m) * a.y_stride + n0 + n) = v;
+      });
 }
 
 }  // namespace
@@ -147,11 +152,15 @@ hipError_t launch_quantize_rows(const QuantizeRows& a, bool f32, hipStream_t s) 
 }
 
 hipError_t launch_quantized_linear(QuantizedLinear a, hipStream_t s) {
-  constexpr int kT = 128;
-  a.tiles_n = (a.N + kT - 1) / kT;
-  hipLaunchKernelGGL((k7_linear<kT, kT, 2, 2, 2>),
-                     dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0, s,
-                     a);
+  auto launch = [&](auto edge) {
+    constexpr int kT = decltype(edge)::value;
+    a.tiles_n = (a.N + kT - 1) / kT;
+    hipLaunchKernelGGL((k7_linear<kT, kT == 256 ? 1 : 2>),
+                       dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0,
+                       s, a);
+  };
+  if (grouped_in_256(a.g, a.N, (a.K + 127) / 128)) launch(std::integral_constant<int, 256>{});
+  else launch(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
 

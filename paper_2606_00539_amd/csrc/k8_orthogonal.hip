@@ -23,78 +23,167 @@ namespace gnmr {
 namespace {
 
 using mm::F16;
+using mm::f32x4;
 using mm::u32x2;
 using mm::u32x4;
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+__device__ __forceinline__ u32x2 half4(float a, float b, float c, float d) {
+  return __builtin_bit_cast(u32x2, f16x4{_Float16(a), _Float16(b), _Float16(c), _Float16(d)});
+}
 
 constexpr float kHeld = 0x1p12f;       // what X, A and B are multiplied by in fp16
 constexpr float kUnheld = 0x1p-12f;
-constexpr int kNormBlocks = 64;        // partial sums of squares of one matrix
 
-__device__ __forceinline__ float value(const void* p, int64_t i, bool f32) {
-  return f32 ? static_cast<const float*>(p)[i]
-             : __uint_as_float(uint32_t(static_cast<const uint16_t*>(p)[i]) << 16);
+// Eight values from p, which is aligned to 16 bytes.
+template <bool kF32>
+__device__ __forceinline__ void eight(const char* p, float* v) {
+  if constexpr (kF32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x4 q = reinterpret_cast<const f32x4*>(p)[h];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[4 * h + k] = q[k];
+    }
+  } else {
+    const u32x4 q = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[2 * k] = __uint_as_float(q[k] << 16);
+      v[2 * k + 1] = __uint_as_float(q[k] & 0xFFFF0000u);
+    }
+  }
+}
+template <bool kF32>
+__device__ __forceinline__ float one_value(const char* p) {
+  if constexpr (kF32) return *reinterpret_cast<const float*>(p);
+  else return __uint_as_float(uint32_t(*reinterpret_cast<const uint16_t*>(p)) << 16);
 }
 
+// Partial sums of squares of each matrix, in float64: a.parts workgroups a matrix.
+template <bool kF32>
 __global__ __launch_bounds__(256) void k8_norm(const Orthogonal a) {
+  constexpr int kSize = kF32 ? 4 : 2;
   __shared__ double red[4];
-  const int64_t size = int64_t(a.rows) * a.cols, at = int64_t(blockIdx.y) * size;
+  const int64_t size = int64_t(a.rows) * a.cols;
+  const char* p = static_cast<const char*>(a.in) + int64_t(blockIdx.y) * size * kSize;
+  // up to the first 16-byte boundary one by one, then eight at a time
+  const int64_t skew = (16 - reinterpret_cast<uintptr_t>(p) % 16) % 16 / kSize;
+  const int64_t head = skew < size ? skew : size, body = (size - head) / 8;
+  const int64_t first = int64_t(blockIdx.x) * 256 + threadIdx.x, all = int64_t(a.parts) * 256;
   double ss = 0.0;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < size; i += kNormBlocks * 256) {
-    const double v = value(a.in, at + i, a.f32);
-    ss = fma(v, v, ss);
+  auto add = [&](float v) { ss = fma(double(v), double(v), ss); };
+  const char* q = p + head * kSize;
+#pragma unroll 4
+  for (int64_t i = first; i < body; i += all) {
+    float v[8];
+    eight<kF32>(q + i * 8 * kSize, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(v[k]);
   }
+  if (first < head) add(one_value<kF32>(p + first * kSize));
+  const int64_t tail = head + 8 * body + first;
+  if (tail < size) add(one_value<kF32>(p + tail * kSize));
   ss = wave_sum(ss);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
   __syncthreads();
   if (threadIdx.x == 0)
-    a.sums[int64_t(blockIdx.y) * kNormBlocks + blockIdx.x] = ((red[0] + red[1]) + red[2]) + red[3];
+    a.sums[int64_t(blockIdx.y) * a.parts + blockIdx.x] = ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-// X (and zeros around it) from G: 64 x 64 elements to a workgroup.
+// X (and zeros around it) from G: 64 x 64 elements to a workgroup.  Reads go along the rows
+// of G and writes along those of X, through LDS where X is the transpose.
+template <bool kF32, bool kFlip>
 __global__ __launch_bounds__(256) void k8_load(const Orthogonal a) {
-  __shared__ float tile[64][65];
+  constexpr int kSize = kF32 ? 4 : 2;
+  __shared__ double red[4];
   const int64_t size = int64_t(a.rows) * a.cols;
   const int mat = blockIdx.z, m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  double ss = a.sums[int64_t(mat) * kNormBlocks + (threadIdx.x & 63)];
+  double ss = 0.0;
+  for (int i = threadIdx.x; i < a.parts; i += 256) ss += a.sums[int64_t(mat) * a.parts + i];
   ss = wave_sum(ss);
-  const double norm = sqrt(ss) + double(a.eps);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+  __syncthreads();
+  const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]) + double(a.eps);
   int k = 0;
   (void)frexp(norm, &k);            // norm = f * 2^k, f in [0.5, 1)
   const int up = 12 - k;            // |G| * 2^up <= 2^12
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
     a.factor[mat] = norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, up));
-  const char* in = static_cast<const char*>(a.in) + int64_t(mat) * size * (a.f32 ? 4 : 2);
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  for (int i = ty; i < 64; i += 4) {
-    // reads go along the rows of G
-    const int r = a.flip ? n0 + i : m0 + i, c = a.flip ? m0 + tx : n0 + tx;
-    float v = 0.0f;
-    if (r < a.rows && c < a.cols) v = value(in, int64_t(r) * a.cols + c, a.f32);
-    if (a.flip) tile[tx][i] = v;
-    else tile[i][tx] = v;
-  }
-  __syncthreads();
+  // eight consecutive elements of a row of G to a lane: rows r0 .. r0+63 from column c0
+  const char* in = static_cast<const char*>(a.in) + int64_t(mat) * size * kSize;
+  const int r0 = kFlip ? n0 : m0, c0 = kFlip ? m0 : n0;
+  const bool vectors = a.cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.in) % 16 == 0;
   _Float16* x = a.x[0] + int64_t(mat) * a.mp * a.np;
-  for (int i = ty; i < 64; i += 4)
-    x[int64_t(m0 + i) * a.np + n0 + tx] = _Float16(ldexpf(tile[i][tx], up));
+  __shared__ _Float16 tile[kFlip ? 64 : 1][72];
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+    const int i = 32 * pass + (threadIdx.x >> 3), j = 8 * (threadIdx.x & 7);
+    const int r = r0 + i, c = c0 + j;
+    float v[8] = {};
+    if (r < a.rows) {
+      const char* p = in + (int64_t(r) * a.cols + c) * kSize;
+      if (vectors) {
+        if (c < a.cols) eight<kF32>(p, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < a.cols) v[e] = one_value<kF32>(p + e * kSize);
+      }
+    }
+    _Float16 h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = _Float16(ldexpf(v[e], up));
+    if constexpr (kFlip) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[j + e][i] = h[e];
+    } else {
+      *reinterpret_cast<u32x4*>(x + int64_t(m0 + i) * a.np + n0 + j) =
+          *reinterpret_cast<const u32x4*>(h);
+    }
+  }
+  if constexpr (kFlip) {
+    __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+      const int i = 32 * pass + (threadIdx.x >> 3), j = 8 * (threadIdx.x & 7);
+      *reinterpret_cast<u32x4*>(x + int64_t(m0 + i) * a.np + n0 + j) =
+          *reinterpret_cast<const u32x4*>(&tile[i][j]);
+    }
+  }
 }
 
 enum { kGram, kPoly, kApply, kLast };
 
 // One product of an iteration: A = X X^T; B = b A + c A A; X = a X + B X; the last X.
-template <int kWhat, bool kFlip, int kT, int kStages, int kPerCu>
-__global__ __launch_bounds__(mm::kThreads, kPerCu) void k8_product(const Orthogonal a) {
+// A and B are symmetric: their tiles above the diagonal are computed and leave twice.
+template <int kWhat, bool kFlip, int kT>
+__global__ __launch_bounds__(mm::kThreads, kT == 256 ? 1 : 2) void k8_product(const Orthogonal a) {
   constexpr bool kIntoX = kWhat == kApply || kWhat == kLast;
-  using T = mm::Tile<F16, false, kIntoX, kT, kT, 2, kStages>;
+  using D = mm::Depth<false, kIntoX>;
+  using T = mm::Tile<F16, false, kIntoX, kT, kT, 2, D::kStep, D::kStages, kFlip>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = a.tiles_m * a.tiles_n, v = xcd_order(blockIdx.x, a.count * per);
-  const int mat = v / per;
+  int v = xcd_order(blockIdx.x, a.num_tiles), part = 0;
+  if constexpr (kT == 128) {
+    part = v & 3;
+    v >>= 2;
+  }
+  v += a.first_tile;
+  const int mat = v / a.tiles;
   int tm, tn;
-  walk<8>(v % per, a.tiles_m, a.tiles_n, &tm, &tn);
+  if constexpr (kIntoX) walk<8>(v % a.tiles, a.tiles_m, a.tiles_n, &tm, &tn);
+  else walk_triangle(v % a.tiles, &tm, &tn);
+  if constexpr (kT == 128) {
+    tm = 2 * tm + (part >> 1);
+    tn = 2 * tn + (part & 1);
+  }
   const int m0 = tm * kT, n0 = tn * kT;
+  if (m0 >= a.mp || n0 >= (kIntoX ? a.np : a.mp) || (!kIntoX && tm > tn)) return;
   const int N = kIntoX ? a.np : a.mp, K = kWhat == kGram ? a.np : a.mp;
   const _Float16* x = a.x[a.now] + int64_t(mat) * a.mp * a.np;
   _Float16* A = a.A + int64_t(mat) * a.mp * a.mp;
@@ -108,61 +197,117 @@ __global__ __launch_bounds__(mm::kThreads, kPerCu) void k8_product(const Orthogo
   om.at(left + int64_t(m0) * ld, int64_t(ld) * 2, a.mp - m0, wave, lane);
   if constexpr (kIntoX) on.at(right + n0, int64_t(a.np) * 2, a.np - n0, wave, lane);
   else on.at(right + int64_t(n0) * ld, int64_t(ld) * 2, a.mp - n0, wave, lane);
-  T::template product<kFlip>(acc, om, on, K, wave, lane);
+  T::product(acc, om, on, K, wave, lane);
   const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * what is held
-  T::template each<kFlip>(wave, lane, [&](int i, int j, int g, int dm, int dn) {
-    const int m = m0 + dm, n = n0 + dn;
-    const auto& c = acc[i][j];
-    if constexpr (kWhat == kGram) {
-      if (m < a.mp && n < a.mp) {
-        f16x4 h;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) h[k] = _Float16(c[4 * g + k] * (f * f * kHeld));
-        *reinterpret_cast<f16x4*>(A + int64_t(m) * a.mp + n) = h;
-      }
-    } else if constexpr (kWhat == kPoly) {
-      if (m < a.mp && n < a.mp) {
-        const f16x4 old = *reinterpret_cast<const f16x4*>(A + int64_t(m) * a.mp + n);
-        f16x4 h;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          h[k] = _Float16(a.cb * float(old[k]) + (a.cc * kUnheld) * c[4 * g + k]);
-        *reinterpret_cast<f16x4*>(B + int64_t(m) * a.mp + n) = h;
-      }
-    } else if constexpr (kWhat == kApply) {
+  if constexpr (!kIntoX) {
+    _Float16* to = kWhat == kGram ? A : B;
+    const float s = f * f * kHeld, p = a.cb, q = a.cc * kUnheld;
+    T::change(acc, wave, lane, [&](int m, int n, f32x4 c) {
+      if constexpr (kWhat == kGram) return c * s;
+      const f16x4 old = *reinterpret_cast<const f16x4*>(
+          A + int64_t(min(m0 + m, a.mp - 1)) * a.mp + min(n0 + n, a.mp - 4));
+      return f32x4{p * float(old[0]) + q * c[0], p * float(old[1]) + q * c[1],
+                   p * float(old[2]) + q * c[2], p * float(old[3]) + q * c[3]};
+    });
+    auto round = [](int, int, float a0, float a1, float a2, float a3) {
+      return half4(a0, a1, a2, a3);
+    };
+    T::out16(acc, wave, lane, round, [&](int m, int n, const u32x4& h) {
+      if (m0 + m < a.mp && n0 + n < a.mp)
+        *reinterpret_cast<u32x4*>(to + int64_t(m0 + m) * a.mp + n0 + n) = h;
+    });
+    if (tm == tn) return;
+    T::out16_mirrored(acc, wave, lane, round, [&](int n, int m, const u32x4& h) {
+      if (m0 + m < a.mp && n0 + n < a.mp)
+        *reinterpret_cast<u32x4*>(to + int64_t(n0 + n) * a.mp + m0 + m) = h;
+    });
+  } else if constexpr (kWhat == kApply) {
+    _Float16* to = a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np;
+    const float p = a.ca * (f * kHeld), q = f;
+    const int n = n0 + T::col(wave, lane);
+    T::out32(acc, wave, lane, [&](int e, const f32x4& c) {
+      const int m = m0 + T::row(e, wave, lane);
       if (m < a.mp && n < N) {
-        const f16x4 old = *reinterpret_cast<const f16x4*>(x + int64_t(m) * a.np + n);
-        f16x4 h;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          h[k] = _Float16((a.ca * float(old[k]) + kUnheld * c[4 * g + k]) * (f * kHeld));
-        *reinterpret_cast<f16x4*>(a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np +
-                                  int64_t(m) * a.np + n) = h;
+        const int64_t at = int64_t(m) * N + n;
+        const f16x4 old = *reinterpret_cast<const f16x4*>(x + at);
+        *reinterpret_cast<u32x2*>(to + at) =
+            half4(p * float(old[0]) + q * c[0], p * float(old[1]) + q * c[1],
+                  p * float(old[2]) + q * c[2], p * float(old[3]) + q * c[3]);
       }
-    } else {
-      // four elements along m with kFlip, along n without
-      __bf16* out = a.out + int64_t(mat) * a.m * a.n;
+    });
+  } else {
+    // rows of the update: m, or n with kFlip
+    const int rows = kFlip ? a.n : a.m, cols = kFlip ? a.m : a.n;
+    const int row0 = kFlip ? n0 : m0, col0 = kFlip ? m0 : n0;
+    __bf16* out = a.out + int64_t(mat) * a.m * a.n;
+    const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
+    const float p = a.ca * (f * a.scale), q = kUnheld * (f * a.scale);
+    T::out16(
+        acc, wave, lane,
+        [&](int row, int col, float a0, float a1, float a2, float a3) {
+          const int r = row0 + row, c = col0 + col;
+          float old[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int mk = kFlip ? m + k : m, nk = kFlip ? n : n + k;
-        if (mk < a.m && nk < a.n) {
-          const float old = float(x[int64_t(mk) * a.np + nk]);
-          const float r = (a.ca * old + kUnheld * c[4 * g + k]) * (f * a.scale);
-          out[kFlip ? int64_t(nk) * a.m + mk : int64_t(mk) * a.n + nk] = __bf16(r);
-        }
-      }
-    }
-  });
+          for (int k = 0; k < 4; ++k) {
+            const int m = kFlip ? c + k : r, n = kFlip ? r : c + k;
+            old[k] = float(x[int64_t(min(m, a.mp - 1)) * a.np + min(n, a.np - 1)]);
+          }
+          return u32x2{pack(p * old[0] + q * a0, p * old[1] + q * a1),
+                       pack(p * old[2] + q * a2, p * old[3] + q * a3)};
+        },
+        [&](int row, int col, const u32x4& h) {
+          const int r = row0 + row, c = col0 + col;
+          if (r >= rows || c >= cols) return;
+          __bf16* to = out + int64_t(r) * cols + c;
+          if (whole) {
+            *reinterpret_cast<u32x4*>(to) = h;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (c + k < cols)
+                to[k] = __builtin_bit_cast(__bf16, uint16_t(h[k >> 1] >> (16 * (k & 1))));
+          }
+        });
+  }
 }
 
+// Tiles [first, first + n) of 256 x 256 in the order of the walk, as such or (kT = 128) as their
+// quarters.
+template <int kWhat, bool kFlip, int kT>
+void launch_tiles(Orthogonal a, int64_t first, int64_t n, hipStream_t s) {
+  a.first_tile = int32_t(first);
+  a.num_tiles = int32_t(kT == 256 ? n : 4 * n);
+  if (n > 0)
+    hipLaunchKernelGGL((k8_product<kWhat, kFlip, kT>), dim3(unsigned(a.num_tiles)),
+                       dim3(mm::kThreads), 0, s, a);
+}
+
+// A product's tiles: rounds of 256 over the chip in 256 tiles, and the last round that would
+// not fill it, or all, in 128 tiles, whichever takes the least by us_of_256 and us_of_128.
 template <int kWhat, bool kFlip>
 void launch_product(Orthogonal a, hipStream_t s) {
-  constexpr int kT = 128;
-  a.tiles_m = (a.mp + kT - 1) / kT;
-  a.tiles_n = ((kWhat == kGram || kWhat == kPoly ? a.mp : a.np) + kT - 1) / kT;
-  hipLaunchKernelGGL((k8_product<kWhat, kFlip, kT, 2, 2>),
-                     dim3(unsigned(int64_t(a.count) * a.tiles_m * a.tiles_n)), dim3(mm::kThreads),
-                     0, s, a);
+  constexpr bool kSquare = kWhat == kGram || kWhat == kPoly;
+  a.tiles_m = (a.mp + 255) / 256;
+  a.tiles_n = kSquare ? a.tiles_m : (a.np + 255) / 256;
+  a.tiles = kSquare ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
+  const int64_t all = int64_t(a.count) * a.tiles;
+  const double steps = (kWhat == kGram ? a.np : a.mp) / 64;
+  // 128 tiles that lie in the product
+  const double m = (a.mp + 127) / 128, n = (a.np + 127) / 128;
+  const double small = a.count * (kSquare ? m * (m + 1) / 2 : m * n);
+  const int64_t rest = all % 256;
+  double best = us_of_256(double(all), steps);
+  int64_t in256 = all;
+  if (us_of_128(small, steps) < best) {
+    best = us_of_128(small, steps);
+    in256 = 0;
+  }
+  constexpr double kLaunch = 4.0;
+  const double split = us_of_256(double(all - rest), steps) + kLaunch +
+                       us_of_128(small * double(rest) / double(all), steps);
+  if (all > rest && split < best) in256 = all - rest;
+  launch_tiles<kWhat, kFlip, 256>(a, 0, in256, s);
+  launch_tiles<kWhat, kFlip, 128>(a, in256, all - in256, s);
 }
 
 int pad(int x) { return (x + 63) / 64 * 64; }
@@ -175,10 +320,21 @@ int64_t orthogonal_workgroups(const Orthogonal& a) {
   return a.count * ((mp + 127) / 128) * ((np + 127) / 128);
 }
 
+namespace {
+
+// Workgroups that sum one matrix's squares: enough for the chip over all matrices, at
+// least 8,192 values each.
+int norm_parts(int64_t size, int count) {
+  const int64_t most = std::max<int64_t>(1, 1024 / count);
+  return int(std::min(most, (size + 8191) / 8192));
+}
+
+}  // namespace
+
 int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count) {
   const int64_t mp = pad(std::min(rows, cols)), np = pad(std::max(rows, cols));
-  return up256(int64_t(count) * kNormBlocks * 8) + up256(int64_t(count) * 4) +
-         int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
+  return up256(int64_t(count) * norm_parts(int64_t(rows) * cols, count) * 8) +
+         up256(int64_t(count) * 4) + int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
 }
 
 hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream_t s) {
@@ -189,7 +345,8 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   a.np = pad(a.n);
   char* w = static_cast<char*>(workspace);
   a.sums = reinterpret_cast<double*>(w);
-  w += up256(int64_t(a.count) * kNormBlocks * 8);
+  a.parts = norm_parts(int64_t(a.rows) * a.cols, a.count);
+  w += up256(int64_t(a.count) * a.parts * 8);
   a.factor = reinterpret_cast<float*>(w);
   w += up256(int64_t(a.count) * 4);
   const int64_t xs = int64_t(a.count) * a.mp * a.np, as = int64_t(a.count) * a.mp * a.mp;
@@ -197,9 +354,14 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   a.x[1] = a.x[0] + xs;
   a.A = a.x[1] + xs;
   a.B = a.A + as;
-  hipLaunchKernelGGL(k8_norm, dim3(kNormBlocks, unsigned(a.count)), dim3(256), 0, s, a);
-  hipLaunchKernelGGL(k8_load, dim3(unsigned(a.np / 64), unsigned(a.mp / 64), unsigned(a.count)),
-                     dim3(256), 0, s, a);
+  const dim3 parts(unsigned(a.parts), unsigned(a.count));
+  const dim3 tiles(unsigned(a.np / 64), unsigned(a.mp / 64), unsigned(a.count));
+  if (a.f32) hipLaunchKernelGGL(k8_norm<true>, parts, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k8_norm<false>, parts, dim3(256), 0, s, a);
+  if (a.f32 && a.flip) hipLaunchKernelGGL((k8_load<true, true>), tiles, dim3(256), 0, s, a);
+  else if (a.f32) hipLaunchKernelGGL((k8_load<true, false>), tiles, dim3(256), 0, s, a);
+  else if (a.flip) hipLaunchKernelGGL((k8_load<false, true>), tiles, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k8_load<false, false>), tiles, dim3(256), 0, s, a);
   for (int i = 0; i < steps; ++i) {
     a.first = i == 0;
     a.now = i & 1;

@@ -26,8 +26,13 @@
 #define ENTRIES(X)                                                             \
   X(gnmr_step) X(gnmr_step_from_norms) X(gnmr_step_from_partials) X(gnmr_sumsq) \
   X(gnmr_actuate) X(gnmr_actuate_matrix) X(gnmr_wgrad_sumsq) X(gnmr_wgrad_sumsq_batched)
+/* the expert step's, bound apart (bind_experts) */
+#define EXPERT_ENTRIES(X)                                             \
+  X(gnmr_grouped_linear) X(gnmr_grouped_dgrad) X(gnmr_grouped_wgrad) \
+  X(gnmr_quantize_rows) X(gnmr_quantized_linear) X(gnmr_orthogonalize)
 #define DECLARE(f) static __typeof__(&f) p_##f;
 ENTRIES(DECLARE)
+EXPERT_ENTRIES(DECLARE)
 
 static PyObject *s_data_ptr, *s_cuda_stream, *s_value;
 
@@ -323,12 +328,118 @@ static PyObject* wgrad_sumsq_batched(PyObject* m, PyObject* const* a, Py_ssize_t
   return PyLong_FromLong(status);
 }
 
-/* bind({name: address}): where the entry points are */
-static PyObject* bind(PyObject* m, PyObject* const* a, Py_ssize_t n) {
-  if (n != 1 || !PyDict_Check(a[0])) {
-    PyErr_SetString(PyExc_TypeError, "bind() takes a dict of addresses");
+/* -- the expert step's operators ------------------------------------------------ */
+
+static int as_ptr_or_null(PyObject* o, void** p) {
+  *p = NULL;
+  return o == Py_None ? 0 : as_ptr(o, p);
+}
+
+/* a[0..4]: rows, groups, offsets or None, mask or None, mask value */
+static int as_groups(PyObject* const* a, gnmr_groups* g) {
+  void *off, *mask;
+  if (as_i64(a[0], &g->rows) || as_i32(a[1], &g->num_groups) || as_ptr_or_null(a[2], &off) ||
+      as_ptr_or_null(a[3], &mask) || as_i32(a[4], &g->mask_value))
+    return -1;
+  g->offsets = off;
+  g->d_mask = mask;
+  return 0;
+}
+
+static PyObject* grouped_rows(PyObject* const* a, Py_ssize_t n, __typeof__(&gnmr_grouped_linear) f) {
+  gnmr_groups g;
+  void *in, *w, *out, *stream;
+  int64_t in_stride, out_stride;
+  int32_t outf, inf;
+  if (arity(n, 13) || as_groups(a, &g) || as_ptr(a[5], &in) || as_i64(a[6], &in_stride) ||
+      as_ptr(a[7], &w) || as_ptr(a[8], &out) || as_i64(a[9], &out_stride) || as_i32(a[10], &outf) ||
+      as_i32(a[11], &inf) || as_stream(a[12], &stream))
     return NULL;
-  }
+  CALL(f(&g, in, in_stride, w, out, out_stride, outf, inf, stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* grouped_linear(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return grouped_rows(a, n, p_gnmr_grouped_linear);
+}
+
+static PyObject* grouped_dgrad(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  return grouped_rows(a, n, p_gnmr_grouped_dgrad);
+}
+
+static PyObject* grouped_wgrad(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  gnmr_groups g;
+  void *dy, *x, *dw, *parts, *stream;
+  int64_t dy_stride, x_stride;
+  int32_t dtype, accumulate, outf, inf;
+  if (arity(n, 16) || as_groups(a, &g) || as_ptr(a[5], &dy) || as_i64(a[6], &dy_stride) ||
+      as_ptr(a[7], &x) || as_i64(a[8], &x_stride) || as_ptr(a[9], &dw) || as_i32(a[10], &dtype) ||
+      as_i32(a[11], &accumulate) || as_ptr(a[12], &parts) || as_i32(a[13], &outf) ||
+      as_i32(a[14], &inf) || as_stream(a[15], &stream))
+    return NULL;
+  CALL(p_gnmr_grouped_wgrad(&g, dy, dy_stride, x, x_stride, dw, dtype, accumulate, parts, outf, inf,
+                            stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* quantize_rows(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *x, *codes, *scale, *stream;
+  int64_t x_stride, rows;
+  int32_t dtype, cols;
+  if (arity(n, 8) || as_ptr(a[0], &x) || as_i32(a[1], &dtype) || as_i64(a[2], &x_stride) ||
+      as_ptr(a[3], &codes) || as_ptr(a[4], &scale) || as_i64(a[5], &rows) ||
+      as_i32(a[6], &cols) || as_stream(a[7], &stream))
+    return NULL;
+  CALL(p_gnmr_quantize_rows(x, dtype, x_stride, codes, scale, rows, cols, stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* quantized_linear(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  gnmr_groups g;
+  void *x, *x_scale, *codes, *w_scale, *y, *work, *stream;
+  int64_t x_stride, y_stride, bytes;
+  int32_t outf, inf;
+  if (arity(n, 17) || as_groups(a, &g) || as_ptr(a[5], &x) || as_i64(a[6], &x_stride) ||
+      as_ptr_or_null(a[7], &x_scale) || as_ptr(a[8], &codes) || as_ptr(a[9], &w_scale) ||
+      as_ptr(a[10], &y) || as_i64(a[11], &y_stride) || as_i32(a[12], &outf) ||
+      as_i32(a[13], &inf) || as_ptr_or_null(a[14], &work) || as_i64(a[15], &bytes) ||
+      as_stream(a[16], &stream))
+    return NULL;
+  CALL(p_gnmr_quantized_linear(&g, x, x_stride, x_scale, codes, w_scale, y, y_stride, outf, inf,
+                               work, bytes, stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* orthogonalize(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *in, *out, *work, *stream;
+  gnmr_newton_schulz z;
+  int32_t dtype, rows, cols, count;
+  int64_t bytes;
+  double v[5];
+  if (arity(n, 15) || as_ptr(a[0], &in) || as_i32(a[1], &dtype) || as_ptr(a[2], &out) ||
+      as_i32(a[3], &rows) || as_i32(a[4], &cols) || as_i32(a[5], &count) ||
+      as_i32(a[6], &z.steps) || as_f64(a[7], v) || as_f64(a[8], v + 1) || as_f64(a[9], v + 2) ||
+      as_f64(a[10], v + 3) || as_f64(a[11], v + 4) || as_ptr_or_null(a[12], &work) ||
+      as_i64(a[13], &bytes) || as_stream(a[14], &stream))
+    return NULL;
+  z.a = (float)v[0];
+  z.b = (float)v[1];
+  z.c = (float)v[2];
+  z.eps = (float)v[3];
+  z.scale = (float)v[4];
+  CALL(p_gnmr_orthogonalize(in, dtype, out, rows, cols, count, &z, work, bytes, stream))
+  return PyLong_FromLong(status);
+}
+
+/* bind({name: address}): where the entry points are; bind_experts the same of the others */
+static int is_dict(PyObject* const* a, Py_ssize_t n) {
+  if (n == 1 && PyDict_Check(a[0])) return 1;
+  PyErr_SetString(PyExc_TypeError, "bind() takes a dict of addresses");
+  return 0;
+}
+
+static PyObject* bind(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  if (!is_dict(a, n)) return NULL;
 #define ADDRESS(f)                                                        \
   uint64_t u_##f;                                                         \
   {                                                                       \
@@ -345,6 +456,13 @@ static PyObject* bind(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+static PyObject* bind_experts(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  if (!is_dict(a, n)) return NULL;
+  EXPERT_ENTRIES(ADDRESS)
+  EXPERT_ENTRIES(STORE)
+  Py_RETURN_NONE;
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef kMethods[] = {METHOD(bind),
                                  METHOD(step),
@@ -355,6 +473,13 @@ static PyMethodDef kMethods[] = {METHOD(bind),
                                  METHOD(actuate_matrix),
                                  METHOD(wgrad_sumsq),
                                  METHOD(wgrad_sumsq_batched),
+                                 METHOD(bind_experts),
+                                 METHOD(grouped_linear),
+                                 METHOD(grouped_dgrad),
+                                 METHOD(grouped_wgrad),
+                                 METHOD(quantize_rows),
+                                 METHOD(quantized_linear),
+                                 METHOD(orthogonalize),
                                  {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, kMethods,
                                      NULL, NULL, NULL, NULL};

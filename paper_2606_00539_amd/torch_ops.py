@@ -16,11 +16,14 @@ torch_experts.py does that).
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.GNMR_BF16, torch.float32: B.GNMR_F32}
+_num_partials = functools.lru_cache(None)(B.gnmr_grouped_wgrad_num_partials)
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
@@ -78,8 +81,29 @@ def _output(out, mask, rows, cols, like):
     return out
 
 
+class _Here:
+    """The context of a call on the current device (torch.cuda.device takes longer than
+    a small call's marshalling)."""
+
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_HERE = _Here()
+# the handle alone, without the object around it that takes ten times as long to make
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _on(t):
-    return torch.cuda.device(t.device), torch.cuda.current_stream(t.device).cuda_stream
+    """(context, stream): t's device made current, and torch's current stream on it."""
+    index = t.device.index
+    if index == torch.cuda.current_device():
+        return _HERE, _raw_stream(index)
+    return torch.cuda.device(index), _raw_stream(index)
 
 
 def grouped_linear(x, w, offsets=None, mask=None, mask_value=1, out=None):
@@ -132,7 +156,7 @@ def grouped_wgrad(dy, x, offsets=None, mask=None, mask_value=1, dw=None, accumul
         dw = torch.empty(E, o, i, dtype=dtype, device=dy.device)
     elif dw.shape != (E, o, i) or dw.dtype not in _DTYPES or not dw.is_contiguous():
         raise TypeError(f"dw must be a contiguous bf16 or fp32 tensor of shape {(E, o, i)}")
-    n = B.gnmr_grouped_wgrad_num_partials(o, i)
+    n = _num_partials(o, i)
     if partials is None:
         if mask is not None:
             raise ValueError("with a mask, partials is needed: the other experts' stay in it")
