@@ -225,7 +225,7 @@ struct Orthogonal {
   double* sums;           // [count][parts], partial sums of squares
   float* factor;          // [count], first iteration: X = factor * what is held
   _Float16* x[2];         // [count][mp][np]
-  _Float16 *A, *B;        // [count][mp][mp]
+  _Float16 *A, *P;        // [count][mp][mp]
 };
 int64_t orthogonal_workgroups(const Orthogonal& a);
 int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count);

@@ -116,26 +116,49 @@ __device__ __forceinline__ bool find_row_tile(const GroupArgs& g, int tiles_n, i
   return false;
 }
 
-// Microseconds that tiles of 256 x 256 (one workgroup per CU) or 128 x 128 (two per CU) take,
-// `steps` K steps of 128 bytes each, with the whole chip at work.  A 256 tile does twice as much
-// per byte that passes the L1 (the 128 tile's bound: its 32 KiB a step take as long as its
-// matrix-core work), but there are a quarter as many.  Measured a step and beside them: 1.45 and
-// 9 us; 1.05 (two at once; 0.6 alone on a CU) and 8 us.
-inline double us_of_256(double tiles, double steps) {
-  return ceil(tiles / 256.0) * (1.45 * steps + 9.0);
-}
-inline double us_of_128(double tiles, double steps) {
-  const double rest = tiles - 512.0 * floor(tiles / 512.0);
-  return floor(tiles / 512.0) * (1.05 * steps + 8.0) +
-         (rest <= 0.0 ? 0.0 : (rest <= 256.0 ? 0.6 : 1.05) * steps + 8.0);
+// Microseconds that `tiles` tiles of kT x kT take, `steps` K steps of 128 bytes each, where the
+// product touches `bytes` of memory.  A 256 tile (one to a CU) does twice as much per byte that
+// passes the L1 as a 128 tile (two to a CU), whose bound that is (its 32 KiB a step take as long
+// there as its matrix-core work), and a 64 tile (two to a CU) a quarter; but of the smaller ones
+// there are 4 and 16 times as many to spread over the chip.  Fitted to products of 128 G x 128 G
+// x K, us in tiles of 64 / 128 / 256:
+//   K        512               2048              8192
+//   G = 4    9.1  9.1  14.3    9.0 14.9  36.0    25  74 127
+//   G = 11   8.6  8.4  15.0   14.0 22.5  38.0    47  76 128
+//   G = 16  11.7  8.6  15.5   27.0 24.0  39.0    90  74 130
+//   G = 22  19.5 17.5  16.9   48.4 31.6  40.3   178 110 134
+//   G = 32  37.1 23.4  30.3   96.1 62.0  56.3   366 223 192
+//   G = 45  71.7 41.7  53.8  195  119   142     730 437 491
+// and to what the memory-side cache cannot hold, where a 128 tile's step takes longer and a 256
+// tile's does not: 24,576 rows, 2048 to 1408, in 1, 32 and 64 groups 146, 174 and 194, and 154,
+// 159 and 181; 64 products 1408 x 1408 x 2048 633 and 549.
+template <int kT>
+double us_of_tiles(double tiles, double steps, double bytes) {
+  constexpr double kRound = kT == 256 ? 256 : 512;  // tiles that run at once
+  constexpr double kCacheBytes = 256e6;
+  const double rounds = floor(tiles / kRound), rest = tiles - rounds * kRound;
+  if (kT == 256)  // (with few tiles the clock is higher)
+    return rounds * (1.35 * steps + 16.0) +
+           (rest <= 0.0 ? 0.0 : (0.95 + 0.48 * rest / 256.0) * steps + 8.0);
+  const double two = kT == 64 ? 0.31 : bytes > kCacheBytes ? 1.08 : 0.84;
+  const double alone = kT == 64 ? 0.15 : 0.53;
+  return rounds * (two * steps + 5.0) +
+         (rest <= 0.0 ? 0.0 : (rest <= 256.0 ? alone : two) * steps + 6.0);
 }
 
-// Whether a grouped product over `rows` rows and N columns runs in 256 tiles.  The groups' sizes
-// are not known here: each is taken to leave half a tile empty.
-inline bool grouped_in_256(const GroupArgs& g, int N, double steps) {
-  const double empty = g.offsets == nullptr ? 0.0 : 0.5 * std::min<double>(g.num, g.rows);
-  auto tiles = [&](double t) { return ceil(g.rows / t + empty) * ceil(N / t); };
-  return us_of_256(tiles(256.0), steps) < us_of_128(tiles(128.0), steps);
+// The tile edge of a product of grouped rows, N columns and `steps` K steps, whose weights have
+// `weight` bytes a value.  The groups' sizes are not known here: each is taken to leave half a
+// tile empty.
+inline int grouped_tile(const GroupArgs& g, int N, int K, int weight) {
+  const double rows = g.rows, steps = ceil(double(K) * weight / 128.0);
+  const double used = std::min<double>(g.num, rows);  // groups with rows, at most
+  const double empty = g.offsets == nullptr ? 0.0 : 0.5 * used;
+  const double bytes = rows * (double(K) * weight + 2.0 * N) + used * N * double(K) * weight;
+  auto tiles = [&](double t) { return ceil(rows / t + empty) * ceil(N / t); };
+  const double us64 = us_of_tiles<64>(tiles(64.0), steps, bytes);
+  const double us128 = us_of_tiles<128>(tiles(128.0), steps, bytes);
+  const double us256 = us_of_tiles<256>(tiles(256.0), steps, bytes);
+  return us64 <= us128 && us64 <= us256 ? 64 : us128 <= us256 ? 128 : 256;
 }
 
 // Tiles of kT rows that `rows` rows in g.num groups (and the rest) can make at most.

@@ -32,9 +32,9 @@ __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 1
 __device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 
 // linear (kDgrad false) and dgrad: out[t][n] = sum_k in[t][k] * W_e(n, k).
-template <bool kDgrad, int kT, int kPerCu>
-__global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_rows(const GroupedRows a) {
-  using D = mm::Depth<false, kDgrad>;
+template <bool kDgrad, int kT>
+__global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, kDgrad, kT>::kPerCu)) void k6_rows(const GroupedRows a) {
+  using D = mm::Depth<false, kDgrad, kT>;
   using T = mm::Tile<Bf16, false, kDgrad, kT, kT, 2, D::kStep, D::kStages>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(mm::kThreads, kPerCu) void k6_rows(const GroupedRow
 // 334 and 365, accumulating 536 and 431.
 template <bool kF32, bool kAcc, int kT>
 struct WgradTile {
-  static constexpr int kPerCu = kT == 256 ? 1 : kF32 && kAcc ? 2 : 3;
+  static constexpr int kPerCu = kT == 256 ? 1 : kAcc ? 2 : 3;
   using T = mm::Tile<Bf16, true, true, kT, kT, 2, 64, kPerCu == 3 ? 3 : 4>;
 };
 
@@ -94,14 +94,15 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
   Old old[kEarly ? T::kPieces : 1];
   const int col = T::col(wave, lane);
   auto there = [&](int row) { return m0 + row < a.M && n0 + col < a.N; };
+  // (rows and columns past the last ones read those)
+  const int last = a.M - 1 - m0, edge = min(col, a.N - n0 - 4);
   auto stored = [&](int row) {
-    return static_cast<char*>(a.dw) + (base + int64_t(row) * a.N + col) * (kF32 ? 4 : 2);
+    return static_cast<char*>(a.dw) + (base + int64_t(min(row, last)) * a.N + edge) * (kF32 ? 4 : 2);
   };
   if constexpr (kEarly) {
 #pragma unroll
     for (int q = 0; q < T::kPieces; ++q) {
-      const int row = T::row(q, wave, lane);
-      old[q] = there(row) ? *reinterpret_cast<const Old*>(stored(row)) : Old{};
+      old[q] = *reinterpret_cast<const Old*>(stored(T::row(q, wave, lane)));
     }
   }
   T::product(acc, om, on, end - begin, wave, lane);
@@ -125,25 +126,30 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
           }
         });
   } else {
-    T::out32(acc, wave, lane, [&](int q, f32x4 v) {
-      const int row = T::row(q, wave, lane);
-      if (!there(row)) return;
-      Old* p = reinterpret_cast<Old*>(stored(row));
-      Old was{};
-      if constexpr (kEarly) was = old[q];
-      else if constexpr (kAcc) was = *p;
-      if constexpr (kF32) {
-        if constexpr (kAcc) v += was;
-        *p = v;
-      } else {
-        const u32x2 r{pack(v[0] + low(was.x), v[1] + high(was.x)),
-                      pack(v[2] + low(was.y), v[3] + high(was.y))};
-        *p = r;
-        v = f32x4{low(r.x), high(r.x), low(r.y), high(r.y)};
-      }
+    T::out32(
+        acc, wave, lane,
+        [&](int q) {
+          if constexpr (kAcc && !kEarly)
+            return *reinterpret_cast<const Old*>(stored(T::row(q, wave, lane)));
+          else return Old{};
+        },
+        [&](int q, f32x4 v, Old was) {
+          const int row = T::row(q, wave, lane);
+          if (!there(row)) return;
+          Old* p = reinterpret_cast<Old*>(stored(row));
+          if constexpr (kEarly) was = old[q];
+          if constexpr (kF32) {
+            if constexpr (kAcc) v += was;
+            *p = v;
+          } else {
+            const u32x2 r{pack(v[0] + low(was.x), v[1] + high(was.x)),
+                          pack(v[2] + low(was.y), v[3] + high(was.y))};
+            *p = r;
+            v = f32x4{low(r.x), high(r.x), low(r.y), high(r.y)};
+          }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) square(v[k]);
-    });
+          for (int k = 0; k < 4; ++k) square(v[k]);
+        });
   }
   ss = wave_sum(ss);
   const int blocks_n = (a.N + kGroupedBlock - 1) / kGroupedBlock;
@@ -164,7 +170,7 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
 template <bool kDgrad, int kT>
 void launch_rows(GroupedRows a, hipStream_t s) {
   a.tiles_n = (a.N + kT - 1) / kT;
-  hipLaunchKernelGGL((k6_rows<kDgrad, kT, kT == 256 ? 1 : 2>),
+  hipLaunchKernelGGL((k6_rows<kDgrad, kT>),
                      dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0, s,
                      a);
 }
@@ -192,15 +198,20 @@ void launch_wgrad_of(GroupedWgrad a, hipStream_t s) {
 }  // namespace
 
 int64_t grouped_rows_workgroups(const GroupedRows& a) {
-  return most_row_tiles(a.g, 128) * ((a.N + 127) / 128);
+  return most_row_tiles(a.g, 64) * ((a.N + 63) / 64);
 }
 
 hipError_t launch_grouped_rows(const GroupedRows& a, bool dgrad, hipStream_t s) {
-  const bool large = grouped_in_256(a.g, a.N, (a.K + 63) / 64);
-  if (dgrad && large) launch_rows<true, 256>(a, s);
-  else if (dgrad) launch_rows<true, 128>(a, s);
-  else if (large) launch_rows<false, 256>(a, s);
-  else launch_rows<false, 128>(a, s);
+  const int tile = grouped_tile(a.g, a.N, a.K, 2);
+  if (dgrad) {
+    if (tile == 64) launch_rows<true, 64>(a, s);
+    else if (tile == 128) launch_rows<true, 128>(a, s);
+    else launch_rows<true, 256>(a, s);
+  } else {
+    if (tile == 64) launch_rows<false, 64>(a, s);
+    else if (tile == 128) launch_rows<false, 128>(a, s);
+    else launch_rows<false, 256>(a, s);
+  }
   return hipGetLastError();
 }
 

@@ -102,9 +102,9 @@ __global__ __launch_bounds__(256) void k7_quantize(const QuantizeRows a) {
     *reinterpret_cast<u32x2*>(q + i) = codes(eight<kF32>(x, i), inv);
 }
 
-template <int kT, int kPerCu>
-__global__ __launch_bounds__(mm::kThreads, kPerCu) void k7_linear(const QuantizedLinear a) {
-  using D = mm::Depth<false, false>;
+template <int kT>
+__global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, false, kT>::kPerCu)) void k7_linear(const QuantizedLinear a) {
+  using D = mm::Depth<false, false, kT>;
   using T = mm::Tile<Int8, false, false, kT, kT, 2, D::kStep, D::kStages>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(mm::kThreads, kPerCu) void k7_linear(const Quantize
 int64_t quantized_codes_stride(int32_t in_features) { return (int64_t(in_features) + 15) / 16 * 16; }
 
 int64_t quantized_linear_workgroups(const GroupArgs& g, int32_t out_features) {
-  return most_row_tiles(g, 128) * ((out_features + 127) / 128);
+  return most_row_tiles(g, 64) * ((out_features + 63) / 64);
 }
 
 hipError_t launch_quantize_rows(const QuantizeRows& a, bool f32, hipStream_t s) {
@@ -155,12 +155,14 @@ hipError_t launch_quantized_linear(QuantizedLinear a, hipStream_t s) {
   auto launch = [&](auto edge) {
     constexpr int kT = decltype(edge)::value;
     a.tiles_n = (a.N + kT - 1) / kT;
-    hipLaunchKernelGGL((k7_linear<kT, kT == 256 ? 1 : 2>),
+    hipLaunchKernelGGL((k7_linear<kT>),
                        dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0,
                        s, a);
   };
-  if (grouped_in_256(a.g, a.N, (a.K + 127) / 128)) launch(std::integral_constant<int, 256>{});
-  else launch(std::integral_constant<int, 128>{});
+  const int tile = grouped_tile(a.g, a.N, a.K, 1);
+  if (tile == 64) launch(std::integral_constant<int, 64>{});
+  else if (tile == 128) launch(std::integral_constant<int, 128>{});
+  else launch(std::integral_constant<int, 256>{});
   return hipGetLastError();
 }
 

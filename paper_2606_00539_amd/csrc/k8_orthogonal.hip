@@ -2,18 +2,21 @@
 // where needed), many of one shape at a time:
 //
 //   X = G / (||G||_F + eps)
-//   repeat `steps` times:  A = X X^T,  B = b A + c A A,  X = a X + B X
+//   repeat `steps` times:  A = X X^T,  P = a I + b A + c A A,  X = P X
 //   out = scale * X
 //
 // drives every singular value of G towards 1 and keeps its singular vectors.
 //
 // The iterates are held in fp16 between the products, scaled by 2^12: |X| <= its
-// largest singular value, which the usual coefficients keep below 1.3, so the range
-// holds values from 2^-26 (with all 11 bits) to 16, and each product's rounding is
-// 2^-12 relative, an eighth of bf16's at the same matrix-core rate.  Products
-// accumulate in fp32 and a X is added in fp32.  The first X is G times a power of
-// two, exact for bf16 input; what is left of the norm goes into the first
-// iteration's factors.  The norm is summed in float64.
+// largest singular value, which the usual coefficients keep below 1.3 (and |P| below
+// 4), so the range holds values from 2^-26 (with all 11 bits) to 16, and each product's
+// rounding is 2^-12 relative, an eighth of bf16's at the same matrix-core rate.  Products
+// accumulate in fp32.  a is part of P's diagonal and is rounded with it, to 2^-12
+// of at most a: as much again as X's own rounding, and less than the error of the
+// result in bf16; added to the product in fp32 it would cost a read of X for every
+// product (64 updates of 1408 x 2048: 640 us a product, 540 without).  The first X is
+// G times a power of two, exact for bf16 input; what is left of the norm goes into the
+// first iteration's factors.  The norm is summed in float64.
 #include "gnmr_internal.h"
 #include "groups.h"
 #include "lane_ops.h"
@@ -37,7 +40,7 @@ __device__ __forceinline__ u32x2 half4(float a, float b, float c, float d) {
   return __builtin_bit_cast(u32x2, f16x4{_Float16(a), _Float16(b), _Float16(c), _Float16(d)});
 }
 
-constexpr float kHeld = 0x1p12f;       // what X, A and B are multiplied by in fp16
+constexpr float kHeld = 0x1p12f;       // what X, A and P are multiplied by in fp16
 constexpr float kUnheld = 0x1p-12f;
 
 // Eight values from p, which is aligned to 16 bytes.
@@ -158,37 +161,39 @@ __global__ __launch_bounds__(256) void k8_load(const Orthogonal a) {
   }
 }
 
-enum { kGram, kPoly, kApply, kLast };
+enum { kGram, kPoly, kApply, kLast };  // the products of an iteration; the last X
 
-// One product of an iteration: A = X X^T; B = b A + c A A; X = a X + B X; the last X.
-// A and B are symmetric: their tiles above the diagonal are computed and leave twice.
+// One product: A = X X^T; P = a I + b A + c A A; X = P X, or the result from it.
+// A and P are symmetric: their tiles above the diagonal are computed and leave twice.
 template <int kWhat, bool kFlip, int kT>
-__global__ __launch_bounds__(mm::kThreads, kT == 256 ? 1 : 2) void k8_product(const Orthogonal a) {
+__global__ __launch_bounds__(
+    mm::kThreads, (mm::Depth<false, kWhat == kApply || kWhat == kLast, kT>::kPerCu)) void k8_product(const Orthogonal a) {
   constexpr bool kIntoX = kWhat == kApply || kWhat == kLast;
-  using D = mm::Depth<false, kIntoX>;
+  using D = mm::Depth<false, kIntoX, kT>;
   using T = mm::Tile<F16, false, kIntoX, kT, kT, 2, D::kStep, D::kStages, kFlip>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int v = xcd_order(blockIdx.x, a.num_tiles), part = 0;
-  if constexpr (kT == 128) {
-    part = v & 3;
-    v >>= 2;
+  constexpr int kSide = 256 / kT;
+  if constexpr (kT < 256) {
+    part = v % (kSide * kSide);
+    v /= kSide * kSide;
   }
   v += a.first_tile;
   const int mat = v / a.tiles;
   int tm, tn;
   if constexpr (kIntoX) walk<8>(v % a.tiles, a.tiles_m, a.tiles_n, &tm, &tn);
   else walk_triangle(v % a.tiles, &tm, &tn);
-  if constexpr (kT == 128) {
-    tm = 2 * tm + (part >> 1);
-    tn = 2 * tn + (part & 1);
+  if constexpr (kT < 256) {
+    tm = kSide * tm + part / kSide;
+    tn = kSide * tn + part % kSide;
   }
   const int m0 = tm * kT, n0 = tn * kT;
   if (m0 >= a.mp || n0 >= (kIntoX ? a.np : a.mp) || (!kIntoX && tm > tn)) return;
-  const int N = kIntoX ? a.np : a.mp, K = kWhat == kGram ? a.np : a.mp;
+  const int K = kWhat == kGram ? a.np : a.mp;
   const _Float16* x = a.x[a.now] + int64_t(mat) * a.mp * a.np;
   _Float16* A = a.A + int64_t(mat) * a.mp * a.mp;
-  _Float16* B = a.B + int64_t(mat) * a.mp * a.mp;
-  const _Float16* left = kWhat == kGram ? x : kWhat == kPoly ? A : B;
+  _Float16* P = a.P + int64_t(mat) * a.mp * a.mp;
+  const _Float16* left = kWhat == kGram ? x : kWhat == kPoly ? A : P;
   const _Float16* right = kWhat == kPoly ? A : x;
   const int ld = kWhat == kGram ? a.np : a.mp;
   typename T::Acc acc[T::kBM][T::kBN];
@@ -200,14 +205,17 @@ __global__ __launch_bounds__(mm::kThreads, kT == 256 ? 1 : 2) void k8_product(co
   T::product(acc, om, on, K, wave, lane);
   const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * what is held
   if constexpr (!kIntoX) {
-    _Float16* to = kWhat == kGram ? A : B;
-    const float s = f * f * kHeld, p = a.cb, q = a.cc * kUnheld;
+    _Float16* to = kWhat == kGram ? A : P;
+    const float s = f * f * kHeld, p = a.cb, q = a.cc * kUnheld, one = a.ca * kHeld;
     T::change(acc, wave, lane, [&](int m, int n, f32x4 c) {
       if constexpr (kWhat == kGram) return c * s;
       const f16x4 old = *reinterpret_cast<const f16x4*>(
           A + int64_t(min(m0 + m, a.mp - 1)) * a.mp + min(n0 + n, a.mp - 4));
-      return f32x4{p * float(old[0]) + q * c[0], p * float(old[1]) + q * c[1],
-                   p * float(old[2]) + q * c[2], p * float(old[3]) + q * c[3]};
+      f32x4 r;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        r[k] = p * float(old[k]) + q * c[k] + (m0 + m == n0 + n + k ? one : 0.0f);
+      return r;
     });
     auto round = [](int, int, float a0, float a1, float a2, float a3) {
       return half4(a0, a1, a2, a3);
@@ -223,37 +231,26 @@ __global__ __launch_bounds__(mm::kThreads, kT == 256 ? 1 : 2) void k8_product(co
     });
   } else if constexpr (kWhat == kApply) {
     _Float16* to = a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np;
-    const float p = a.ca * (f * kHeld), q = f;
-    const int n = n0 + T::col(wave, lane);
-    T::out32(acc, wave, lane, [&](int e, const f32x4& c) {
-      const int m = m0 + T::row(e, wave, lane);
-      if (m < a.mp && n < N) {
-        const int64_t at = int64_t(m) * N + n;
-        const f16x4 old = *reinterpret_cast<const f16x4*>(x + at);
-        *reinterpret_cast<u32x2*>(to + at) =
-            half4(p * float(old[0]) + q * c[0], p * float(old[1]) + q * c[1],
-                  p * float(old[2]) + q * c[2], p * float(old[3]) + q * c[3]);
-      }
-    });
+    T::out16(
+        acc, wave, lane,
+        [&](int, int, float a0, float a1, float a2, float a3) {
+          return half4(f * a0, f * a1, f * a2, f * a3);
+        },
+        [&](int m, int n, const u32x4& h) {
+          if (m0 + m < a.mp && n0 + n < a.np)
+            *reinterpret_cast<u32x4*>(to + int64_t(m0 + m) * a.np + n0 + n) = h;
+        });
   } else {
     // rows of the update: m, or n with kFlip
     const int rows = kFlip ? a.n : a.m, cols = kFlip ? a.m : a.n;
     const int row0 = kFlip ? n0 : m0, col0 = kFlip ? m0 : n0;
     __bf16* out = a.out + int64_t(mat) * a.m * a.n;
     const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-    const float p = a.ca * (f * a.scale), q = kUnheld * (f * a.scale);
+    const float s = kUnheld * (f * a.scale);
     T::out16(
         acc, wave, lane,
-        [&](int row, int col, float a0, float a1, float a2, float a3) {
-          const int r = row0 + row, c = col0 + col;
-          float old[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int m = kFlip ? c + k : r, n = kFlip ? r : c + k;
-            old[k] = float(x[int64_t(min(m, a.mp - 1)) * a.np + min(n, a.np - 1)]);
-          }
-          return u32x2{pack(p * old[0] + q * a0, p * old[1] + q * a1),
-                       pack(p * old[2] + q * a2, p * old[3] + q * a3)};
+        [&](int, int, float a0, float a1, float a2, float a3) {
+          return u32x2{pack(s * a0, s * a1), pack(s * a2, s * a3)};
         },
         [&](int row, int col, const u32x4& h) {
           const int r = row0 + row, c = col0 + col;
@@ -271,43 +268,46 @@ __global__ __launch_bounds__(mm::kThreads, kT == 256 ? 1 : 2) void k8_product(co
   }
 }
 
-// Tiles [first, first + n) of 256 x 256 in the order of the walk, as such or (kT = 128) as their
-// quarters.
+// Tiles [first, first + n) of 256 x 256 in the order of the walk, as such or cut into smaller ones.
 template <int kWhat, bool kFlip, int kT>
 void launch_tiles(Orthogonal a, int64_t first, int64_t n, hipStream_t s) {
+  if (n == 0) return;
   a.first_tile = int32_t(first);
-  a.num_tiles = int32_t(kT == 256 ? n : 4 * n);
-  if (n > 0)
-    hipLaunchKernelGGL((k8_product<kWhat, kFlip, kT>), dim3(unsigned(a.num_tiles)),
-                       dim3(mm::kThreads), 0, s, a);
+  a.num_tiles = int32_t(n * (256 / kT) * (256 / kT));
+  hipLaunchKernelGGL((k8_product<kWhat, kFlip, kT>), dim3(unsigned(a.num_tiles)),
+                     dim3(mm::kThreads), 0, s, a);
 }
 
-// A product's tiles: rounds of 256 over the chip in 256 tiles, and the last round that would
-// not fill it, or all, in 128 tiles, whichever takes the least by us_of_256 and us_of_128.
+// A product's tiles: all of one edge, or 256 tiles in whole rounds over the chip and the rest,
+// which would not fill another, in smaller ones; whichever takes the least by us_of_tiles.
 template <int kWhat, bool kFlip>
 void launch_product(Orthogonal a, hipStream_t s) {
   constexpr bool kSquare = kWhat == kGram || kWhat == kPoly;
   a.tiles_m = (a.mp + 255) / 256;
   a.tiles_n = kSquare ? a.tiles_m : (a.np + 255) / 256;
   a.tiles = kSquare ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
-  const int64_t all = int64_t(a.count) * a.tiles;
+  const int64_t all = int64_t(a.count) * a.tiles, rest = all % 256;
   const double steps = (kWhat == kGram ? a.np : a.mp) / 64;
-  // 128 tiles that lie in the product
-  const double m = (a.mp + 127) / 128, n = (a.np + 127) / 128;
-  const double small = a.count * (kSquare ? m * (m + 1) / 2 : m * n);
-  const int64_t rest = all % 256;
-  double best = us_of_256(double(all), steps);
-  int64_t in256 = all;
-  if (us_of_128(small, steps) < best) {
-    best = us_of_128(small, steps);
-    in256 = 0;
-  }
-  constexpr double kLaunch = 4.0;
-  const double split = us_of_256(double(all - rest), steps) + kLaunch +
-                       us_of_128(small * double(rest) / double(all), steps);
-  if (all > rest && split < best) in256 = all - rest;
-  launch_tiles<kWhat, kFlip, 256>(a, 0, in256, s);
-  launch_tiles<kWhat, kFlip, 128>(a, in256, all - in256, s);
+  // smaller tiles that lie in the product, the share of them in the rest
+  auto tiles = [&](double t) {
+    const double m = ceil(a.mp / t), n = ceil(a.np / t);
+    return a.count * (kSquare ? m * (m + 1) / 2 : m * n);
+  };
+  const double share = double(rest) / double(all), kLaunch = 4.0;
+  const double bytes = 2.0 * a.count * a.mp * (kWhat == kGram   ? a.np + a.mp
+                                                  : kWhat == kPoly ? 2.0 * a.mp
+                                                                   : a.mp + 2.0 * a.np);
+  const double whole = us_of_tiles<256>(double(all - rest), steps, bytes) + kLaunch;
+  const double us[5] = {us_of_tiles<64>(tiles(64.0), steps, bytes),
+                        us_of_tiles<128>(tiles(128.0), steps, bytes),
+                        us_of_tiles<256>(double(all), steps, bytes),
+                        whole + us_of_tiles<64>(share * tiles(64.0), steps, bytes),
+                        whole + us_of_tiles<128>(share * tiles(128.0), steps, bytes)};
+  const int best = int(std::min_element(us, us + (rest < all && rest > 0 ? 5 : 3)) - us);
+  const int64_t large = best < 2 ? 0 : best == 2 ? all : all - rest;
+  launch_tiles<kWhat, kFlip, 256>(a, 0, large, s);
+  if (best == 0 || best == 3) launch_tiles<kWhat, kFlip, 64>(a, large, all - large, s);
+  else launch_tiles<kWhat, kFlip, 128>(a, large, all - large, s);
 }
 
 int pad(int x) { return (x + 63) / 64 * 64; }
@@ -317,7 +317,7 @@ int64_t up256(int64_t x) { return (x + 255) / 256 * 256; }
 
 int64_t orthogonal_workgroups(const Orthogonal& a) {
   const int64_t mp = pad(std::min(a.rows, a.cols)), np = pad(std::max(a.rows, a.cols));
-  return a.count * ((mp + 127) / 128) * ((np + 127) / 128);
+  return a.count * ((mp + 255) / 256) * ((np + 255) / 256) * 16;  // in tiles of 64
 }
 
 namespace {
@@ -353,7 +353,7 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   a.x[0] = reinterpret_cast<_Float16*>(w);
   a.x[1] = a.x[0] + xs;
   a.A = a.x[1] + xs;
-  a.B = a.A + as;
+  a.P = a.A + as;
   const dim3 parts(unsigned(a.parts), unsigned(a.count));
   const dim3 tiles(unsigned(a.np / 64), unsigned(a.mp / 64), unsigned(a.count));
   if (a.f32) hipLaunchKernelGGL(k8_norm<true>, parts, dim3(256), 0, s, a);

@@ -78,7 +78,7 @@ __device__ __forceinline__ void meet() {
 template <class E, bool kCols, int kT, int kStep>
 struct Operand {
   static_assert(!kCols || E::kBytes == 2, "k as the slow index: 16-bit types only");
-  static_assert(!kCols || kT >= 128, "the swizzle of a cols operand takes eight units a row");
+  static_assert(!kCols || kT >= 64, "the swizzle of a cols operand takes four units a row");
   static constexpr int kStepK = kStep / E::kBytes;       // k per step
   static constexpr int kBytes = kT * kStep;              // of a stage in LDS
   static constexpr int kLoads = kBytes / 1024 / kWaves;  // instructions per wavefront and step
@@ -97,10 +97,10 @@ struct Operand {
     return (row / (16 / kChunks)) & (kChunks - 1);
   }
 
-  // 32-byte units of a cols row: the four k rows and two units that 32 lanes of a
-  // transposing read touch lie in different banks.
+  // 32-byte unit u of row k of a cols stage lies in place u ^ swizzle(k): the four k rows and
+  // two units that 32 lanes of a transposing read touch fill all banks.
   static __device__ __forceinline__ int swizzle(int k) {
-    return (2 * (k & 3)) ^ ((k >> 1) & 1);
+    return kT >= 128 ? (2 * (k & 3)) ^ ((k >> 1) & 1) : k & 2;
   }
 
   __device__ __forceinline__ void at(const void* p, int64_t ld_bytes, int rows, int wave, int lane) {
@@ -205,10 +205,11 @@ struct Reader {
 // lines; where both are "cols" finer steps keep more of them under way in the same LDS:
 // 8192 x 13824 x 5120, us: rows and rows 863 in two steps of 128 bytes, 965 in four of 64;
 // rows and cols 935 and 983; cols and cols 974 and 922.
-template <bool kColsM, bool kColsN>
+template <bool kColsM, bool kColsN, int kT>
 struct Depth {
   static constexpr int kStep = kColsM && kColsN ? 64 : 128;
-  static constexpr int kStages = kColsM && kColsN ? 4 : 2;
+  static constexpr int kStages = (kColsM && kColsN) ? 4 : kT == 64 ? 4 : 2;
+  static constexpr int kPerCu = kT == 256 ? 1 : 2;
 };
 
 // kTM x kTN tiles by kWM x (4 / kWM) wavefronts.  kSwap: accumulator registers hold
@@ -494,17 +495,21 @@ struct Tile {
     return first_col(wave) + 4 * (lane % kChunks32);
   }
 
-  // The same with the accumulators as they are: put(e, v) gets piece e.
-  template <class Put>
+  // The same with the accumulators as they are: put(e, v, w) gets piece e and what fetch(e) made.
+  // All of a pass's fetches (loads from memory) are on their way before its first put.
+  template <class Fetch, class Put>
   static __device__ __forceinline__ void out32(const Acc (&acc)[kBM][kBN], int wave, int lane,
-                                               Put&& put) {
+                                               Fetch&& fetch, Put&& put) {
     constexpr int kRowBytes = kCols * 4;
-    constexpr int kPass = pass(kRowBytes);
+    constexpr int kPass = pass(kRowBytes), kAtOnce = 32 * kPass / kAtOnce32;
     static_assert(kRows / 32 % kPass == 0 && kPass * 32 * kRowBytes <= kRegion, "whole passes");
     char* const at = region(wave);
     meet();
 #pragma unroll
-    for (int p = 0; p < kRows / 32; p += kPass) {
+    for (int p = 0; p < kRows / 32 / kPass; ++p) {
+      decltype(fetch(0)) had[kAtOnce];
+#pragma unroll
+      for (int e = 0; e < kAtOnce; ++e) had[e] = fetch(p * kAtOnce + e);
 #pragma unroll
       for (int i = 0; i < kPass; ++i)
 #pragma unroll
@@ -512,15 +517,16 @@ struct Tile {
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int row = 32 * i + (lane & 31), col = 32 * j + 8 * g + 4 * (lane >> 5);
-            const Acc& a = kSwap ? acc[j][p + i] : acc[p + i][j];
+            const Acc& a = kSwap ? acc[j][p * kPass + i] : acc[p * kPass + i][j];
             *reinterpret_cast<f32x4*>(chunk<kRowBytes>(at, row, col / 4)) =
                 f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]};
           }
 #pragma unroll
-      for (int r = 0; r < 32 * kPass; r += kAtOnce32)
-        put((32 * p + r) / kAtOnce32,
+      for (int e = 0; e < kAtOnce; ++e)
+        put(p * kAtOnce + e,
             *reinterpret_cast<const f32x4*>(
-                chunk<kRowBytes>(at, r + lane / kChunks32, lane % kChunks32)));
+                chunk<kRowBytes>(at, e * kAtOnce32 + lane / kChunks32, lane % kChunks32)),
+            had[e]);
     }
   }
 };
