@@ -242,6 +242,18 @@ gnmr_status gnmr_quantized_linear(const gnmr_groups* groups, const void* x, int6
         (x_scale == nullptr && rows > kMaxWorkgroups))
       return fail(GNMR_E_INVALID, "too many output tiles for one launch");
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (x_scale == nullptr && gnmr::quantized_token(a.g, in_features)) {
+      const gnmr::QuantizedToken one{static_cast<const uint16_t*>(x),
+                                     static_cast<const int8_t*>(codes),
+                                     w_scale,
+                                     static_cast<uint16_t*>(y),
+                                     a.g.mask,
+                                     a.g.mask_value,
+                                     out_features,
+                                     in_features};
+      GNMR_HIP(gnmr::launch_quantized_token(one, st));
+      return GNMR_OK;
+    }
     a.w = static_cast<const int8_t*>(codes);
     a.w_scale = w_scale;
     a.y = static_cast<uint16_t*>(y);

@@ -206,6 +206,17 @@ struct QuantizedLinear {
   int64_t q_stride, y_stride;
   int32_t N, K, tiles_n;
 };
+struct QuantizedToken {
+  const uint16_t* x;      // [K] bf16
+  const int8_t* w;        // [N][K]
+  const float* w_scale;   // [N]
+  uint16_t* y;            // [N]
+  const uint8_t* mask;    // as GroupArgs
+  int32_t mask_value, N, K;
+};
+// Whether a bf16 x goes through the kernel of one row.
+bool quantized_token(const GroupArgs& g, int32_t in_features);
+hipError_t launch_quantized_token(const QuantizedToken& a, hipStream_t s);
 int64_t quantized_codes_stride(int32_t in_features);
 int64_t quantized_linear_workgroups(const GroupArgs& g, int32_t out_features);
 hipError_t launch_quantize_rows(const QuantizeRows& a, bool f32, hipStream_t s);

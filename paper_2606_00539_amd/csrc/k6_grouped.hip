@@ -170,9 +170,8 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
 template <bool kDgrad, int kT>
 void launch_rows(GroupedRows a, hipStream_t s) {
   a.tiles_n = (a.N + kT - 1) / kT;
-  hipLaunchKernelGGL((k6_rows<kDgrad, kT>),
-                     dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0, s,
-                     a);
+  hipLaunchKernelGGL((k6_rows<kDgrad, kT>), dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)),
+                     dim3(mm::kThreads), 0, s, a);
 }
 
 template <bool kF32, bool kAcc>

@@ -15,6 +15,7 @@ namespace gnmr {
 namespace {
 
 using mm::f32x4;
+using mm::i32x4;
 using mm::Int8;
 using mm::u32x2;
 using mm::u32x4;
@@ -81,25 +82,117 @@ __device__ __forceinline__ u32x2 codes(const Eight& e, float inv) {
   return u32x2{r[0], r[1]};
 }
 
-// One workgroup per row.
-template <bool kF32>
+// kLanes lanes to a row: a wavefront (rows of up to 2,048 values, four to a workgroup) or the
+// workgroup.  The second pass over a row meets it in the L1 or L2.
+template <bool kF32, int kLanes>
 __global__ __launch_bounds__(256) void k7_quantize(const QuantizeRows a) {
   __shared__ uint32_t red[4];
-  const int64_t row = blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x % kLanes;
+  const int64_t row = int64_t(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
+  if (kLanes == 64 && row >= a.rows) return;
   const void* x = static_cast<const char*>(a.x) + row * a.x_stride * (kF32 ? 4 : 2);
   uint32_t m = 0;
-  for (int i = 8 * threadIdx.x; i < a.cols; i += 8 * 256) m = largest(eight<kF32>(x, i), m);
+#pragma unroll 4
+  for (int i = 8 * lane; i < a.cols; i += 8 * kLanes) m = largest(eight<kF32>(x, i), m);
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) m = max(m, uint32_t(__shfl_xor(int(m), d)));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = max(max(red[0], red[1]), max(red[2], red[3]));
+  if constexpr (kLanes == 256) {
+    if ((threadIdx.x & 63) == 0) red[wave] = m;
+    __syncthreads();
+    m = max(max(red[0], red[1]), max(red[2], red[3]));
+  }
   float inv, scale;
   row_scale(m, &inv, &scale);
-  if (threadIdx.x == 0) a.scale[row] = scale;
+  if (lane == 0) a.scale[row] = scale;
   int8_t* q = a.codes + row * a.codes_stride;
-  for (int i = 8 * threadIdx.x; i < a.cols; i += 8 * 256)
+#pragma unroll 4
+  for (int i = 8 * lane; i < a.cols; i += 8 * kLanes)
     *reinterpret_cast<u32x2*>(q + i) = codes(eight<kF32>(x, i), inv);
+}
+
+// One row (a decoding step of one sequence), quantised on the way: a workgroup forms its
+// codes in LDS, reading it from the L2 (10 KiB at 5,120 features), while its first weights
+// are on their way; then its wavefronts take kChannels output channels each, a lane 16 bytes of
+// each channel at a time, four products to an instruction.  The weights' bytes bound it: 5,120 to
+// 13,824 features 14.3 us (5 TB/s), in tiles of 64 behind a launch for the codes 16.9; 13,824 to
+// 5,120 16.5 and 26.6.  (Two and four rows took 18.3 and 24.5 so, 17.2 in tiles.)
+constexpr int kChannels = 4, kAhead = 2;  // chunks of each channel on their way at a time
+
+__device__ __forceinline__ int dot16(const i32x4& a, const i32x4& b, int c) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_sdot4(a[k], b[k], c, false);
+  return c;
+}
+
+// 16 weights from p, of which `left` exist (a multiple of 8)
+__device__ __forceinline__ i32x4 weights16(const int8_t* p, int left) {
+  if (left >= 16) return *reinterpret_cast<const i32x4*>(p);
+  if (left <= 0) return i32x4{0, 0, 0, 0};
+  const u32x2 h = *reinterpret_cast<const u32x2*>(p);
+  return i32x4{int(h.x), int(h.y), 0, 0};
+}
+
+__global__ __launch_bounds__(256) void k7_token(const QuantizedToken a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];  // the row, then its codes
+  __shared__ uint32_t red[4];
+  if (a.mask != nullptr && int(a.mask[0] != 0) != a.mask_value) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n0 = (blockIdx.x * 4 + wave) * kChannels;
+  const int chunks = (a.K + 15) / 16;
+  auto fetch = [&](i32x4 (&w)[kAhead][kChannels], int j0) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int c = 0; c < kChannels; ++c) {
+        const int j = j0 + 64 * k, n = min(n0 + c, a.N - 1);
+        w[k][c] = weights16(a.w + int64_t(n) * a.K + 16 * j, a.K - 16 * j);
+      }
+  };
+  i32x4 next[kAhead][kChannels];
+  fetch(next, lane);
+  u32x4* const row = reinterpret_cast<u32x4*>(lds);
+  char* const q = lds + 32 * chunks;
+  uint32_t m = 0;
+  for (int i = tid; i < 2 * chunks; i += 256) {
+    const u32x4 v = 8 * i < a.K ? reinterpret_cast<const u32x4*>(a.x)[i] : u32x4{0, 0, 0, 0};
+    row[i] = v;
+    m = largest(eight<false>(&v, 0), m);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) m = max(m, uint32_t(__shfl_xor(int(m), d)));
+  if (lane == 0) red[wave] = m;
+  __syncthreads();
+  float inv, sx;
+  row_scale(max(max(red[0], red[1]), max(red[2], red[3])), &inv, &sx);
+  for (int i = tid; i < 2 * chunks; i += 256)
+    *reinterpret_cast<u32x2*>(q + 8 * i) = codes(eight<false>(row + i, 0), inv);
+  __syncthreads();
+  int acc[kChannels] = {};
+  for (int j0 = lane; j0 < chunks; j0 += 64 * kAhead) {
+    i32x4 w[kAhead][kChannels];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int c = 0; c < kChannels; ++c) w[k][c] = next[k][c];
+    fetch(next, j0 + 64 * kAhead);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      // (weights past the last chunk are zero: any code does)
+      const i32x4 x = *reinterpret_cast<const i32x4*>(q + 16 * min(j0 + 64 * k, chunks - 1));
+#pragma unroll
+      for (int c = 0; c < kChannels; ++c) acc[c] = dot16(x, w[k][c], acc[c]);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) acc[c] += __shfl_xor(acc[c], d);
+  if (lane == 0 && n0 < a.N) {  // (N is a multiple of 8: all kChannels exist)
+    float v[kChannels];
+#pragma unroll
+    for (int c = 0; c < kChannels; ++c) v[c] = float(acc[c]) * (sx * a.w_scale[n0 + c]);
+    *reinterpret_cast<u32x2*>(a.y + n0) = u32x2{pack(v[0], v[1]), pack(v[2], v[3])};
+  }
 }
 
 template <int kT>
@@ -146,8 +239,26 @@ int64_t quantized_linear_workgroups(const GroupArgs& g, int32_t out_features) {
 
 hipError_t launch_quantize_rows(const QuantizeRows& a, bool f32, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  if (f32) hipLaunchKernelGGL(k7_quantize<true>, dim3(unsigned(a.rows)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k7_quantize<false>, dim3(unsigned(a.rows)), dim3(256), 0, s, a);
+  if (a.cols <= 2048) {
+    const dim3 wgs(unsigned((int64_t(a.rows) + 3) / 4));
+    if (f32) hipLaunchKernelGGL((k7_quantize<true, 64>), wgs, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k7_quantize<false, 64>), wgs, dim3(256), 0, s, a);
+  } else {
+    const dim3 wgs(unsigned(a.rows));
+    if (f32) hipLaunchKernelGGL((k7_quantize<true, 256>), wgs, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k7_quantize<false, 256>), wgs, dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+bool quantized_token(const GroupArgs& g, int32_t in_features) {
+  // row and codes take three bytes a feature of the LDS
+  return g.offsets == nullptr && g.rows == 1 && in_features <= 16384;
+}
+
+hipError_t launch_quantized_token(const QuantizedToken& a, hipStream_t s) {
+  hipLaunchKernelGGL(k7_token, dim3(unsigned((a.N + 4 * kChannels - 1) / (4 * kChannels))),
+                     dim3(256), size_t(48) * ((a.K + 15) / 16), s, a);
   return hipGetLastError();
 }
 

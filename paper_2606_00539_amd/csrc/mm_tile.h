@@ -208,7 +208,7 @@ struct Reader {
 template <bool kColsM, bool kColsN, int kT>
 struct Depth {
   static constexpr int kStep = kColsM && kColsN ? 64 : 128;
-  static constexpr int kStages = (kColsM && kColsN) ? 4 : kT == 64 ? 4 : 2;
+  static constexpr int kStages = (kColsM && kColsN) || kT == 64 ? 4 : 2;
   static constexpr int kPerCu = kT == 256 ? 1 : 2;
 };
 
