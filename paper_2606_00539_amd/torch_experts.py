@@ -1,0 +1,177 @@
+"""A mixture-of-experts layer's matrices as GNMR units, end to end on the expert
+step's kernels: products grouped by expert, the low-cost path in INT8, weight
+gradients with the controller's sums of squares, orthogonalised updates.
+
+Argument marshalling and bookkeeping only: the products, the codes, the norms and
+the updates run in libgnmr.
+"""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from . import torch_ops as ops
+from .binding import GNMR_BUDGET_ACTIVE, Controller, gnmr_grouped_wgrad_num_partials
+from .torch_units import _current
+
+
+class _ExpertLinear(torch.autograd.Function):
+    """y[t] = W_e x[t]: in bf16 for the experts of A_t, in INT8 for the others.  Backward
+    takes the products with the bf16 weights and the bf16 input on both paths (a
+    straight-through gradient)."""
+
+    @staticmethod
+    def forward(ctx, x, weight, offsets, units, k):
+        ctx.save_for_backward(x, weight, offsets)
+        ctx.units, ctx.k = units, k
+        if units.codes[k] is None:
+            return ops.grouped_linear(x, weight, offsets)
+        y = torch.empty(x.shape[0], weight.shape[1], dtype=x.dtype, device=x.device)
+        mask = units.mask(k)
+        ops.grouped_linear(x, weight, offsets, mask=mask, mask_value=1, out=y)
+        ops.quantized_linear(x, *units.codes[k], offsets, mask=mask, mask_value=0, out=y)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, offsets = ctx.saved_tensors
+        if dy.stride(-1) != 1 or dy.stride(0) % 8 or dy.data_ptr() % 16:
+            dy = dy.contiguous()
+        dx = ops.grouped_dgrad(dy, weight, offsets) if ctx.needs_input_grad[0] else None
+        if ctx.needs_input_grad[1]:
+            ctx.units._weight_grad(ctx.k, dy, x, offsets)
+        return dx, None, None, None, None
+
+
+class ExpertUnits:
+    """Expert weights ([experts, out, in] bf16 parameters) as units, one per expert and
+    matrix, named "<name>.<expert>".
+
+    `linear(name, x, offsets)` is the layer: rows of x sorted by expert, expert e's in
+    [offsets[e], offsets[e + 1]) (int32, on the device; a router's output need not come
+    to the host).  With low_cost, experts outside A_t run in INT8 (codes of the weights
+    made by `refresh()`, which an optimiser calls after it has changed them); the
+    controller's mask is read on the device when the kernels run.
+
+    Backward writes the weight gradients itself, into `grads[name]` in grad_dtype,
+    adding over the micro-batches since the last `step()`, and the sums of squares of
+    what it stores; `step()` runs the controller from those.  weight.grad stays None.
+    """
+
+    def __init__(self, named_weights, window: int = 5, max_o: int = 8, lock_len: int = 8,
+                 eps: float = 1e-12, recoverable=None, budget_mode: int = GNMR_BUDGET_ACTIVE,
+                 warmup_steps: int = 0, low_cost: bool = True, grad_dtype=torch.float32,
+                 stream=None):
+        self.names, self.weights, self.unit_names, first, parts = [], [], [], [0], [0]
+        for name, w in named_weights:
+            if w.dim() != 3 or w.dtype != torch.bfloat16 or not w.is_cuda or not w.is_contiguous():
+                raise TypeError(f"{name}: the weight must be a contiguous bf16 [experts, out, in] "
+                                "tensor on a HIP device")
+            E, o, i = w.shape
+            if o % 8 or i % 8:
+                raise ValueError(f"{name}: features must be multiples of 8, got {o}x{i}")
+            self.names.append(name)
+            self.weights.append(w)
+            self.unit_names += [f"{name}.{e}" for e in range(E)]
+            first.append(first[-1] + E)
+            parts.append(parts[-1] + E * gnmr_grouped_wgrad_num_partials(o, i))
+        if not self.weights:
+            raise ValueError("no expert weight given")
+        if grad_dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError("grad_dtype must be torch.bfloat16 or torch.float32")
+        self._index = {n: k for k, n in enumerate(self.names)}
+        self._first, self._parts = first, parts
+        device = self.weights[0].device
+        self.partials = torch.zeros(parts[-1], dtype=torch.float32, device=device)
+        self.grads = {n: torch.empty(w.shape, dtype=grad_dtype, device=device)
+                      for n, w in zip(self.names, self.weights)}
+        self._filled = [False] * len(self.weights)
+        U = first[-1]
+        off = np.zeros(U + 1, np.int64)
+        for k, w in enumerate(self.weights):
+            n = (parts[k + 1] - parts[k]) // w.shape[0]
+            off[first[k] + 1:first[k + 1] + 1] = parts[k] + n * np.arange(1, w.shape[0] + 1)
+        rec = None
+        if recoverable is not None:
+            rec = np.array([1 if recoverable(u) else 0 for u in self.unit_names], np.uint8)
+        self.ctl = Controller(U, window, max_o, lock_len, eps, np.zeros(U + 1, np.int64), [], [],
+                              None, rec, _current(stream), budget_mode, warmup_steps)
+        self.ctl.bind_partials(off)
+        self._mask = torch.as_tensor(_DeviceBytes(self.ctl, U), device=device)
+        self.low_cost = bool(low_cost)
+        self.codes = [None] * len(self.weights)
+        self.refresh()
+
+    def mask(self, k):
+        """The controller's mask over matrix k's experts (device memory of the controller)."""
+        return self._mask[self._first[k]:self._first[k + 1]]
+
+    def refresh(self) -> None:
+        """The weights' INT8 codes again, after the weights have changed."""
+        if self.low_cost:
+            self.codes = [ops.quantize_rows(w.detach()) for w in self.weights]
+
+    def linear(self, name, x, offsets):
+        k = self._index[name]
+        return _ExpertLinear.apply(x, self.weights[k], offsets, self, k)
+
+    def _weight_grad(self, k, dy, x, offsets):
+        E = self.weights[k].shape[0]
+        ops.grouped_wgrad(dy, x, offsets, dw=self.grads[self.names[k]],
+                          accumulate=self._filled[k],
+                          partials=self.partials[self._parts[k]:self._parts[k + 1]].view(E, -1))
+        self._filled[k] = True
+
+    def step(self, alpha_t: float, beta_t: float, stream=None) -> None:
+        """One controller step from the gradients since the last one (asynchronous)."""
+        for n, done in zip(self.names, self._filled):
+            if not done:
+                raise RuntimeError(f"{n}: no gradient was written since the last step")
+        self.ctl.step_from_partials(self.partials, alpha_t, beta_t, _current(stream))
+        self._filled = [False] * len(self.weights)
+
+    def query(self, stream=None) -> dict:
+        out = self.ctl.query(_current(stream))
+        out["units"] = self.unit_names
+        return out
+
+    def recovery_set(self, stream=None) -> list:
+        m = self.ctl.query(_current(stream))["mask"]
+        return [u for u, a in zip(self.unit_names, m) if a]
+
+    def close(self):
+        self._mask = None
+        self.codes = [None] * len(self.weights)
+        self.ctl.close()
+
+
+class _DeviceBytes:
+    """The controller's mask as an array of device bytes; it keeps the controller."""
+
+    def __init__(self, ctl, n):
+        self.ctl = ctl
+        self.__cuda_array_interface__ = {"shape": (n,), "typestr": "|u1", "version": 2,
+                                         "data": (int(ctl.device_outputs()["mask"]), False)}
+
+
+class OrthogonalMomentum:
+    """Updates the weights of ExpertUnits with their orthogonalised momentum: per matrix
+    m = momentum * m + g (fp32), W -= lr * max(1, out / in)^0.5 * orthogonalize(m), all
+    experts of a matrix in one call; then the units' codes are made again."""
+
+    def __init__(self, units, lr: float, momentum: float = 0.95, steps: int = 5,
+                 coefficients=ops.COEFFICIENTS, eps: float = 1e-7):
+        self.units, self.lr, self.momentum = units, float(lr), float(momentum)
+        self.steps, self.coefficients, self.eps = steps, coefficients, eps
+        self.buffers = {n: torch.zeros(g.shape, dtype=torch.float32, device=g.device)
+                        for n, g in units.grads.items()}
+
+    @torch.no_grad()
+    def step(self) -> None:
+        for name, w in zip(self.units.names, self.units.weights):
+            m = self.buffers[name]
+            m.mul_(self.momentum).add_(self.units.grads[name])
+            scale = max(1.0, w.shape[1] / w.shape[2]) ** 0.5
+            w.sub_(ops.orthogonalize(m, self.steps, self.coefficients, self.eps, scale),
+                   alpha=self.lr)
+        self.units.refresh()
