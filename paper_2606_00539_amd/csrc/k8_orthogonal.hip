@@ -202,19 +202,30 @@ __global__ __launch_bounds__(
   om.at(left + int64_t(m0) * ld, int64_t(ld) * 2, a.mp - m0, wave, lane);
   if constexpr (kIntoX) on.at(right + n0, int64_t(a.np) * 2, a.np - n0, wave, lane);
   else on.at(right + int64_t(n0) * ld, int64_t(ld) * 2, a.mp - n0, wave, lane);
+  // P needs this tile of A: in the smaller tiles it is on its way while the product runs (a
+  // 256 tile has no registers for it)
+  auto stored = [&](int m, int n) {
+    return *reinterpret_cast<const f16x4*>(A + int64_t(min(m0 + m, a.mp - 1)) * a.mp +
+                                           min(n0 + n, a.mp - 4));
+  };
+  constexpr bool kEarly = kWhat == kPoly && kT < 256;
+  f16x4 old[kEarly ? T::kGroups : 1];
+  if constexpr (kEarly)
+    T::groups(wave, lane, [&](int e, int m, int n) { old[e] = stored(m, n); });
   T::product(acc, om, on, K, wave, lane);
   const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * what is held
   if constexpr (!kIntoX) {
     _Float16* to = kWhat == kGram ? A : P;
     const float s = f * f * kHeld, p = a.cb, q = a.cc * kUnheld, one = a.ca * kHeld;
-    T::change(acc, wave, lane, [&](int m, int n, f32x4 c) {
+    T::change(acc, wave, lane, [&](int e, int m, int n, f32x4 c) {
       if constexpr (kWhat == kGram) return c * s;
-      const f16x4 old = *reinterpret_cast<const f16x4*>(
-          A + int64_t(min(m0 + m, a.mp - 1)) * a.mp + min(n0 + n, a.mp - 4));
+      f16x4 h;
+      if constexpr (kEarly) h = old[e];
+      else h = stored(m, n);
       f32x4 r;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        r[k] = p * float(old[k]) + q * c[k] + (m0 + m == n0 + n + k ? one : 0.0f);
+        r[k] = p * float(h[k]) + q * c[k] + (m0 + m == n0 + n + k ? one : 0.0f);
       return r;
     });
     auto round = [](int, int, float a0, float a1, float a2, float a3) {

@@ -466,22 +466,30 @@ struct Tile {
     }
   }
 
-  // fn(row, col, a0, a1, a2, a3) changes the four accumulators at row, col .. col+3.
+  // A lane's groups of four accumulators: fn(e, row, col) for group e at row, col .. col+3.
+  static constexpr int kGroups = kRows * kCols / 256;
   template <class Fn>
-  static __device__ __forceinline__ void change(Acc (&acc)[kBM][kBN], int wave, int lane, Fn&& fn) {
+  static __device__ __forceinline__ void groups(int wave, int lane, Fn&& fn) {
     const int r0 = first_row(wave) + (lane & 31), c0 = first_col(wave) + 4 * (lane >> 5);
 #pragma unroll
     for (int i = 0; i < kRows / 32; ++i)
 #pragma unroll
       for (int j = 0; j < kCols / 32; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          Acc& a = kSwap ? acc[j][i] : acc[i][j];
-          const f32x4 v = fn(r0 + 32 * i, c0 + 32 * j + 8 * g,
-                             f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]});
+        for (int g = 0; g < 4; ++g)
+          fn((i * (kCols / 32) + j) * 4 + g, r0 + 32 * i, c0 + 32 * j + 8 * g);
+  }
+
+  // fn(e, row, col, v) gives group e's four accumulators new values.
+  template <class Fn>
+  static __device__ __forceinline__ void change(Acc (&acc)[kBM][kBN], int wave, int lane, Fn&& fn) {
+    groups(wave, lane, [&](int e, int row, int col) {
+      const int i = e / 4 / (kCols / 32), j = e / 4 % (kCols / 32), g = e % 4;
+      Acc& a = kSwap ? acc[j][i] : acc[i][j];
+      const f32x4 v = fn(e, row, col, f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]});
 #pragma unroll
-          for (int k = 0; k < 4; ++k) a[4 * g + k] = v[k];
-        }
+      for (int k = 0; k < 4; ++k) a[4 * g + k] = v[k];
+    });
   }
 
   // Where out32 puts a lane's pieces: piece e of kPieces is four of row row(e), from column
