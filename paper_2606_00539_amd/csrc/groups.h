@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "gnmr_internal.h"
 #include "lane_ops.h"
@@ -63,27 +64,62 @@ struct RowTile {
   int tn;
 };
 
-// The tile of workgroup w among those that have rows; false where there are fewer.
-// Tiles are kT rows high; the rows behind the last group make a group of their own.
-template <int kT>
+// Which of a launch's tiles a kernel takes: all; or of 256 tiles those that make whole rounds over
+// the chip, and the rest, cut into quarters, where the rest is at most half a round.
+enum Share { kAll, kRounds, kRest };
+__host__ __device__ inline int whole_rounds(int tiles) {
+  const int rest = tiles % 256;
+  return rest <= 128 ? tiles - rest : tiles;
+}
+
+// Position of workgroup w in the order of `total` tiles, and for kRest its quarter; false where
+// the kernel's share is smaller.
+template <Share kShare>
+__device__ __forceinline__ bool place_of(int w, int total, int* v, int* part) {
+  const int whole = kShare == kAll ? total : whole_rounds(total);
+  const int mine = kShare == kRest ? 4 * (total - whole) : whole;
+  if (w >= mine) return false;
+  *v = xcd_order(w, mine);
+  *part = 0;
+  if (kShare == kRest) {
+    *part = *v & 3;
+    *v = whole + (*v >> 2);
+  }
+  return true;
+}
+
+// The tile of workgroup w among those that have rows; false where there are fewer.  Tiles
+// are kT rows high; the rows behind the last group make a group of their own.  kRest (kT =
+// 128): quarters of 256 tiles, tiles_n of which lie side by side; a quarter may have no rows.
+template <int kT, Share kShare>
 __device__ __forceinline__ bool find_row_tile(const GroupArgs& g, int tiles_n, int w, int lane,
                                               RowTile* t) {
+  static_assert(kShare != kRest || kT == 128, "quarters of 256 tiles");
+  constexpr int kHigh = kShare == kRest ? 256 : kT;
+  int v, part, tm;
+  auto quarter = [&] {
+    if constexpr (kShare == kRest) {
+      t->row += kT * (part >> 1);
+      t->rows -= kT * (part >> 1);
+      t->tn = 2 * t->tn + (part & 1);
+    }
+    return t->rows > 0;
+  };
   if (g.offsets == nullptr) {
     if (!group_wanted(g, 0)) return false;
-    const int tiles_m = (g.rows + kT - 1) / kT;
-    if (w >= tiles_m * tiles_n) return false;
-    int tm;
-    walk<8>(xcd_order(w, tiles_m * tiles_n), tiles_m, tiles_n, &tm, &t->tn);
+    const int tiles_m = (g.rows + kHigh - 1) / kHigh;
+    if (!place_of<kShare>(w, tiles_m * tiles_n, &v, &part)) return false;
+    walk<8>(v, tiles_m, tiles_n, &tm, &t->tn);
     t->group = 0;
-    t->row = tm * kT;
+    t->row = tm * kHigh;
     t->rows = g.rows - t->row;
-    return true;
+    return quarter();
   }
   // A lane to a group, 64 groups at a time: all tiles counted, then ours looked up.
   auto high = [&](int e, int* begin, int* end) {
     *begin = *end = 0;
     if (e <= g.num && (e == g.num || group_wanted(g, e))) group_rows(g, e, begin, end);
-    return (*end - *begin + kT - 1) / kT;
+    return (*end - *begin + kHigh - 1) / kHigh;
   };
   int begin, end, n = 0, upto = 0, total = 0;
   for (int e0 = 0; e0 <= g.num; e0 += 64) {
@@ -91,8 +127,7 @@ __device__ __forceinline__ bool find_row_tile(const GroupArgs& g, int tiles_n, i
     upto = int(wave_prefix(uint32_t(n)));
     total += int(lane_of(uint32_t(upto), 63));
   }
-  if (w >= total * tiles_n) return false;
-  const int v = xcd_order(w, total * tiles_n);
+  if (!place_of<kShare>(w, total * tiles_n, &v, &part)) return false;
   int before = 0;
   for (int e0 = 0; e0 <= g.num; e0 += 64) {
     if (g.num >= 64) {
@@ -104,12 +139,11 @@ __device__ __forceinline__ bool find_row_tile(const GroupArgs& g, int tiles_n, i
       const int src = __ffsll((unsigned long long)here) - 1;
       const int tiles_m = int(lane_of(uint32_t(n), src));
       const int first = (before + int(lane_of(uint32_t(upto), src)) - tiles_m) * tiles_n;
-      int tm;
       walk<8>(v - first, tiles_m, tiles_n, &tm, &t->tn);
       t->group = e0 + src;
-      t->row = int(lane_of(uint32_t(begin), src)) + tm * kT;
+      t->row = int(lane_of(uint32_t(begin), src)) + tm * kHigh;
       t->rows = int(lane_of(uint32_t(end), src)) - t->row;
-      return true;
+      return quarter();
     }
     before += int(lane_of(uint32_t(upto), 63));
   }
@@ -146,6 +180,12 @@ double us_of_tiles(double tiles, double steps, double bytes) {
          (rest <= 0.0 ? 0.0 : (rest <= 256.0 ? alone : two) * steps + 6.0);
 }
 
+// Whether the last tiles of a launch of 256 tiles get a launch of their own (which ends at once
+// where the groups leave it none, and takes 5 us then): from this many K steps on what it can save
+// outweighs it.  8,191 rows in 8 groups, 11008 to 4096 (576 tiles): 773 us in one launch, 709 in
+// two.
+constexpr int kSplitSteps = 32;
+
 // The tile edge of a product of grouped rows, N columns and `steps` K steps, whose weights have
 // `weight` bytes a value.  The groups' sizes are not known here: each is taken to leave half a
 // tile empty.
@@ -165,6 +205,28 @@ inline int grouped_tile(const GroupArgs& g, int N, int K, int weight) {
 inline int64_t most_row_tiles(const GroupArgs& g, int kT) {
   if (g.offsets == nullptr) return (int64_t(g.rows) + kT - 1) / kT;
   return g.rows / kT + std::min<int64_t>(int64_t(g.num) + 1, g.rows);
+}
+
+// Launches a product of grouped rows and N columns: launch(edge, share, workgroups), with
+// *tiles_n set to the tiles side by side.
+template <class Launch>
+void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* tiles_n,
+                      Launch&& launch) {
+  using std::integral_constant;
+  const int tile = grouped_tile(g, N, K, weight);
+  *tiles_n = (N + tile - 1) / tile;
+  const int64_t most = most_row_tiles(g, tile) * *tiles_n;
+  const integral_constant<Share, kAll> all;
+  if (tile == 64) return launch(integral_constant<int, 64>{}, all, most);
+  if (tile == 128) return launch(integral_constant<int, 128>{}, all, most);
+  // (without offsets the tiles are known here)
+  const bool split = int64_t(K) * weight >= 128 * kSplitSteps &&
+                     (g.offsets != nullptr || whole_rounds(int(most)) < most);
+  if (!split) return launch(integral_constant<int, 256>{}, all, most);
+  if (g.offsets != nullptr || whole_rounds(int(most)) > 0)
+    launch(integral_constant<int, 256>{}, integral_constant<Share, kRounds>{}, most);
+  launch(integral_constant<int, 128>{}, integral_constant<Share, kRest>{},
+         std::min<int64_t>(4 * most, 512));
 }
 
 }  // namespace gnmr

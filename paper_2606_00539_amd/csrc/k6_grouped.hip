@@ -32,14 +32,15 @@ __device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 1
 __device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 
 // linear (kDgrad false) and dgrad: out[t][n] = sum_k in[t][k] * W_e(n, k).
-template <bool kDgrad, int kT>
+template <bool kDgrad, int kT, Share kShare>
 __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, kDgrad, kT>::kPerCu)) void k6_rows(const GroupedRows a) {
   using D = mm::Depth<false, kDgrad, kT>;
   using T = mm::Tile<Bf16, false, kDgrad, kT, kT, 2, D::kStep, D::kStages>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
-  if (!find_row_tile<kT>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  if (!find_row_tile<kT, kShare>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
   const int n0 = t.tn * kT;
+  if (kShare == kRest && n0 >= a.N) return;
   typename T::Acc acc[T::kBM][T::kBN];
   typename T::OpM om;
   typename T::OpN on;
@@ -167,11 +168,13 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
   }
 }
 
-template <bool kDgrad, int kT>
+template <bool kDgrad>
 void launch_rows(GroupedRows a, hipStream_t s) {
-  a.tiles_n = (a.N + kT - 1) / kT;
-  hipLaunchKernelGGL((k6_rows<kDgrad, kT>), dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)),
-                     dim3(mm::kThreads), 0, s, a);
+  auto launch = [&](auto edge, auto share, int64_t wgs) {
+    hipLaunchKernelGGL((k6_rows<kDgrad, decltype(edge)::value, decltype(share)::value>),
+                       dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
+  };
+  launch_row_tiles(a.g, a.N, a.K, 2, &a.tiles_n, launch);
 }
 
 template <bool kF32, bool kAcc>
@@ -201,16 +204,8 @@ int64_t grouped_rows_workgroups(const GroupedRows& a) {
 }
 
 hipError_t launch_grouped_rows(const GroupedRows& a, bool dgrad, hipStream_t s) {
-  const int tile = grouped_tile(a.g, a.N, a.K, 2);
-  if (dgrad) {
-    if (tile == 64) launch_rows<true, 64>(a, s);
-    else if (tile == 128) launch_rows<true, 128>(a, s);
-    else launch_rows<true, 256>(a, s);
-  } else {
-    if (tile == 64) launch_rows<false, 64>(a, s);
-    else if (tile == 128) launch_rows<false, 128>(a, s);
-    else launch_rows<false, 256>(a, s);
-  }
+  if (dgrad) launch_rows<true>(a, s);
+  else launch_rows<false>(a, s);
   return hipGetLastError();
 }
 

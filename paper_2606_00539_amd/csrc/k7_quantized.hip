@@ -195,14 +195,15 @@ __global__ __launch_bounds__(256) void k7_token(const QuantizedToken a) {
   }
 }
 
-template <int kT>
+template <int kT, Share kShare>
 __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, false, kT>::kPerCu)) void k7_linear(const QuantizedLinear a) {
   using D = mm::Depth<false, false, kT>;
   using T = mm::Tile<Int8, false, false, kT, kT, 2, D::kStep, D::kStages>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
-  if (!find_row_tile<kT>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  if (!find_row_tile<kT, kShare>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
   const int n0 = t.tn * kT, e = t.group < a.g.num ? t.group : 0;
+  if (kShare == kRest && n0 >= a.N) return;
   typename T::Acc acc[T::kBM][T::kBN];
   typename T::OpM om;
   typename T::OpN on;
@@ -263,17 +264,11 @@ hipError_t launch_quantized_token(const QuantizedToken& a, hipStream_t s) {
 }
 
 hipError_t launch_quantized_linear(QuantizedLinear a, hipStream_t s) {
-  auto launch = [&](auto edge) {
-    constexpr int kT = decltype(edge)::value;
-    a.tiles_n = (a.N + kT - 1) / kT;
-    hipLaunchKernelGGL((k7_linear<kT>),
-                       dim3(unsigned(most_row_tiles(a.g, kT) * a.tiles_n)), dim3(mm::kThreads), 0,
-                       s, a);
+  auto launch = [&](auto edge, auto share, int64_t wgs) {
+    hipLaunchKernelGGL((k7_linear<decltype(edge)::value, decltype(share)::value>),
+                       dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
   };
-  const int tile = grouped_tile(a.g, a.N, a.K, 1);
-  if (tile == 64) launch(std::integral_constant<int, 64>{});
-  else if (tile == 128) launch(std::integral_constant<int, 128>{});
-  else launch(std::integral_constant<int, 256>{});
+  launch_row_tiles(a.g, a.N, a.K, 1, &a.tiles_n, launch);
   return hipGetLastError();
 }
 

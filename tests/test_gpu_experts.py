@@ -392,6 +392,94 @@ def test_orthogonalize_zero_and_nonfinite():
     assert np.array_equal(host(t.orthogonalize(g))[3], clean[3])
 
 
+# -- sizes that run in 256 tiles ---------------------------------------------------------
+# (references in float64 on the device: the same formulas, one expert at a time)
+
+def _large(torch, seed, counts, i, o, pad=3):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    off = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    rows = int(off[-1]) + pad
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.bfloat16)
+    x, dy, w = r(rows, i), r(rows, o) * 1e-3, r(len(counts), o, i) * i ** -0.5
+    return off.tolist(), torch.from_numpy(off).cuda(), x, dy, w
+
+
+def _close64(torch, got, want, mag, K, rounded=True):
+    slack = (K + 1) * 2.0 ** -23 * mag + (2.0 ** -8 * want.abs() if rounded else 0)
+    assert bool(((got.double() - want).abs() <= slack).all())
+
+
+# loads whose 256 tiles leave a part of a round, and none; widths that end inside a quarter
+@pytest.mark.parametrize("counts,i,o", [((3100, 17, 4800, 0, 1083), 5120, 4216),
+                                        ((4096, 2048, 2048), 4096, 6144),
+                                        ((9001,), 5128, 4224)])
+@pytest.mark.parametrize("which", ["linear", "dgrad", "quantized"])
+def test_grouped_rows_in_large_tiles(which, counts, i, o):
+    torch, t = ops()
+    say("large", which, counts, i, o)
+    off, d_off, x, dy, w = _large(torch, 21, counts, i, o)
+    if len(counts) == 1:
+        x, dy, d_off = x[:off[-1]], dy[:off[-1]], None
+    if which == "quantized":
+        codes, scale = t.quantize_rows(w)
+        q, s = t.quantize_rows(x)
+        y = t.quantized_linear(x, codes, scale, d_off)
+    elif which == "linear":
+        y = t.grouped_linear(x, w, d_off)
+    else:
+        y = t.grouped_dgrad(dy, w, d_off)
+    assert bool((y[off[-1]:] == 0).all())
+    for e, (a, b) in enumerate(zip(off[:-1], off[1:])):
+        if which == "quantized":      # the sums are exact in float64, the rest as the kernel does it
+            total = (q[a:b].double() @ codes[e].double().t()).float()
+            want = (total * (s[a:b, None] * scale[e][None, :])).to(torch.bfloat16)
+            assert bool((y[a:b] == want).all())
+            continue
+        p = (x if which == "linear" else dy)[a:b].double()
+        m = (w[e].t() if which == "linear" else w[e]).double().contiguous()
+        _close64(torch, y[a:b], p @ m, p.abs() @ m.abs(), m.shape[0])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_grouped_wgrad_in_large_tiles(dtype):
+    torch, t = ops()
+    off, d_off, x, dy, _ = _large(torch, 22, (2500, 2047, 0, 4100), 2056, 1544)
+    # four experts of at least 2,048 rows on average and 4 * 7 * 9 tiles
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    dw, parts = t.grouped_wgrad(dy, x, d_off, dtype=dt)
+    old = dw.clone()
+    t.grouped_wgrad(dy, x, d_off, dw=dw, accumulate=True, partials=parts)
+    for e, (a, b) in enumerate(zip(off[:-1], off[1:])):
+        p, r = dy[a:b].double().t().contiguous(), x[a:b].double()
+        want, mag = p @ r, p.abs() @ r.abs()
+        _close64(torch, old[e], want, mag, b - a, dtype == "bf16")
+        _close64(torch, dw[e], want + old[e].double(), mag + old[e].double().abs(), b - a + 1,
+                 dtype == "bf16")
+        sq = dw[e].double().square()
+        sq = torch.nn.functional.pad(sq, (0, -sq.shape[1] % 128, 0, -sq.shape[0] % 128))
+        blocks = sq.view(-(-1544 // 128), 128, -(-2056 // 128), 128).sum((1, 3)).flatten()
+        assert bool(((parts[e].double() - blocks).abs() <= 300 * 2.0 ** -24 * blocks).all())
+
+
+@pytest.mark.parametrize("count,m,n", [(1, 4100, 6001), (1, 6001, 4100), (40, 700, 1300)])
+def test_orthogonalize_in_large_tiles(count, m, n):
+    """The bound of test_orthogonalize."""
+    torch, t = ops()
+    say("orthogonalize", count, m, n)
+    g = torch.Generator(device="cuda").manual_seed(23)
+    x = (torch.randn(count, m, n, generator=g, device="cuda") * 1e-3).to(torch.bfloat16)
+    got = t.orthogonalize(x)
+    for k in range(0, count, 13):
+        v = x[k].double()
+        v = v if m <= n else v.t().contiguous()
+        v = v / (v.square().sum().sqrt() + 1e-7)
+        for _ in range(5):
+            s = v @ v.t().contiguous()
+            v = COEF[0] * v + (COEF[1] * s + COEF[2] * (s @ s)) @ v
+        v = v if m <= n else v.t()
+        assert float((got[k].double() - v).norm()) <= 0.00825 * float(v.norm())
+
+
 # -- streams and graphs ---------------------------------------------------------------
 
 def test_another_stream_and_a_graph():
