@@ -15,6 +15,15 @@ from .binding import GNMR_BUDGET_ACTIVE, Controller, gnmr_grouped_wgrad_num_part
 from .torch_units import _current
 
 
+def _readable(dy):
+    """dy where the kernels can read it.  Autograd may bring any strides and alignment: a sum's
+    gradient has a row stride of 0, a concatenation's starts anywhere (and may be contiguous)."""
+    if (dy.stride(1) == 1 and dy.shape[1] <= dy.stride(0) < 1 << 22 and dy.stride(0) % 8 == 0 and
+            dy.data_ptr() % 16 == 0):
+        return dy
+    return dy.clone(memory_format=torch.contiguous_format)
+
+
 class _ExpertLinear(torch.autograd.Function):
     """y[t] = W_e x[t]: in bf16 for the experts of A_t, in INT8 for the others.  Backward
     takes the products with the bf16 weights and the bf16 input on both paths (a
@@ -35,8 +44,7 @@ class _ExpertLinear(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, weight, offsets = ctx.saved_tensors
-        if dy.stride(-1) != 1 or dy.stride(0) % 8 or dy.data_ptr() % 16:
-            dy = dy.contiguous()
+        dy = _readable(dy)
         dx = ops.grouped_dgrad(dy, weight, offsets) if ctx.needs_input_grad[0] else None
         if ctx.needs_input_grad[1]:
             ctx.units._weight_grad(ctx.k, dy, x, offsets)

@@ -84,6 +84,38 @@ def test_gradients_norms_and_accumulation(grad_dtype):
     units.close()
 
 
+@pytest.mark.parametrize("how", ["sum over rows", "sum", "transposed", "part of a vector",
+                                 "part of rows"])
+def test_gradients_from_any_layout_of_dy(how):
+    """The output's gradient as autograd brings it: broadcast rows, broadcast values, columns
+    first, contiguous at an odd address, rows an odd number of values apart."""
+    torch, units, weight, off, d_off, x, w, _, dev = setup(6, low_cost=False)
+    rng = np.random.default_rng(60)
+    o = w.shape[1]
+    g = X.bf16(rng.standard_normal((len(x), o)).astype(np.float32))
+    xt = dev(x).requires_grad_()
+    y = units.linear("m", xt, d_off)
+    if how == "sum over rows":
+        g[:] = g[:1]
+        y.sum(0).backward(dev(g[0]))
+    elif how == "sum":
+        g[:] = 1.0
+        y.sum().backward()
+    elif how == "transposed":
+        y.t().contiguous().backward(dev(g).t().contiguous())
+    elif how == "part of a vector":
+        torch.cat([y.new_zeros(3), y.flatten()]).backward(
+            dev(np.pad(g.ravel(), (3, 0))))
+    else:
+        torch.cat([y.new_zeros(len(x), 8), y, y.new_zeros(len(x), 1)], 1).backward(
+            dev(np.pad(g, ((0, 0), (8, 1)))))
+    dx, mag = X.grouped_rows(g, w, off)
+    close(xt.grad.float().cpu().numpy(), dx, mag, o)
+    dw, mw = X.grouped_wgrad(g, x, off)
+    close(units.grads["m"].cpu().numpy(), dw, mw, max(np.diff(off)), rounded=False)
+    units.close()
+
+
 def test_gradients_against_differences():
     """Without the low-cost path the function is linear in x and in W: for a step in a random
     direction the change of sum(y * dy) is the gradient times the step, up to the roundings of
