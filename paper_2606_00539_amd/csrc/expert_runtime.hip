@@ -158,7 +158,7 @@ gnmr_status gnmr_grouped_wgrad(const gnmr_groups* groups, const void* dy, int64_
     if (intersect(sw, sp) || intersect(sw, sy) || intersect(sw, sx) || intersect(sp, sy) ||
         intersect(sp, sx))
       return fail(GNMR_E_INVALID, "dw or partials overlaps another buffer");
-    if (a.g.num * blocks > kMaxWorkgroups)
+    if (a.g.num * (blocks + gnmr::kNumXcd) > kMaxWorkgroups)
       return fail(GNMR_E_INVALID, "too many output tiles for one launch");
     a.dy = static_cast<const uint16_t*>(dy);
     a.x = static_cast<const uint16_t*>(x);

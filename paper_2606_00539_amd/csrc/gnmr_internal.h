@@ -173,6 +173,7 @@ struct GroupedRows {
   uint16_t* out;        // [rows][N], out_stride elements apart
   int64_t in_stride, out_stride;
   int32_t N, K, tiles_n;
+  bool past;              // set by the launch: the output is written past the caches
 };
 struct GroupedWgrad {
   GroupArgs g;
@@ -205,6 +206,7 @@ struct QuantizedLinear {
   uint16_t* y;            // [rows][N], y_stride elements apart
   int64_t q_stride, y_stride;
   int32_t N, K, tiles_n;
+  bool past;              // set by the launch: the output is written past the caches
 };
 struct QuantizedToken {
   const uint16_t* x;      // [K] bf16

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, kDgrad, kT>::kPerCu
       },
       [&](int m, int n, const u32x4& v) {
         if (m < t.rows && n0 + n < a.N)
-          *reinterpret_cast<u32x4*>(a.out + int64_t(t.row + m) * a.out_stride + n0 + n) = v;
+          put(reinterpret_cast<u32x4*>(a.out + int64_t(t.row + m) * a.out_stride + n0 + n), v, a.past);
       });
 }
 
@@ -70,16 +70,41 @@ struct WgradTile {
   using T = mm::Tile<Bf16, true, true, kT, kT, 2, 64, kPerCu == 3 ? 3 : 4>;
 };
 
+// Tile *v of group *e for workgroup w, of `num` groups with `per` tiles each.  Where a group has
+// tiles enough, every XCD (workgroups w, w + 8, ... run on one) takes an eighth of each group's, so
+// that groups of many rows keep all of them busy; false where its eighth is a tile shorter.  64
+// experts 2048 x 1408 (176 tiles each), fp32, over two micro-batches of uneven load: with whole
+// groups to an XCD 733 us, with eighths 672; one call of even load 201 and 218.  Four experts of 80 x
+// 136 (2 tiles each) 15.3 and 19.0.
+constexpr int kSharedTiles = 64;
+__host__ __device__ constexpr int slots_of(int num, int per) {
+  constexpr int kXcds = kNumXcd;
+  return num == 1 || per < kSharedTiles ? per : (per + kXcds - 1) / kXcds * kXcds;
+}
+__device__ __forceinline__ bool share_of(int w, int num, int per, int* v, int* e) {
+  if (num == 1 || per < kSharedTiles) {
+    const int at = xcd_order(w, num * per);
+    *e = at / per;
+    *v = at % per;
+    return true;
+  }
+  constexpr int kXcds = kNumXcd;
+  const int slots = slots_of(num, per) / kXcds, i = w / kXcds, at = i % slots;
+  *e = i / slots;
+  const int xcd = (w + *e) % kXcds, q = per / kXcds, r = per % kXcds;
+  *v = xcd * q + min(xcd, r) + at;
+  return at < q + (xcd < r ? 1 : 0);
+}
+
 template <bool kF32, bool kAcc, int kT>
 __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) void k6_wgrad(
     const GroupedWgrad a) {
   using T = typename WgradTile<kF32, kAcc, kT>::T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = a.tiles_m * a.tiles_n, v = xcd_order(blockIdx.x, a.g.num * per);
-  const int e = v / per;
-  if (!group_wanted(a.g, e)) return;
+  int v, e;
+  if (!share_of(blockIdx.x, a.g.num, a.tiles_m * a.tiles_n, &v, &e) || !group_wanted(a.g, e)) return;
   int tm, tn, begin, end;
-  walk<8>(v % per, a.tiles_m, a.tiles_n, &tm, &tn);
+  walk<8>(v, a.tiles_m, a.tiles_n, &tm, &tn);
   group_rows(a.g, e, &begin, &end);
   const int m0 = tm * kT, n0 = tn * kT;
   typename T::Acc acc[T::kBM][T::kBN];
@@ -115,10 +140,14 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
         [](int, int, float a0, float a1, float a2, float a3) {
           return u32x2{pack(a0, a1), pack(a2, a3)};
         },
+        // Gradients that nothing was added to go past the caches: what they would drive out is dy and
+        // x.  64 and 24 experts 2048 x 1408 of 384 rows, us through and past them: fp32 313 and 201, 110
+        // and 74, bf16 227 and 163, 67 and 65; with a pass that reads the gradient behind it fp32 554
+        // and 522.  (Where experts have a row or two, 13% slower.)  Accumulated ones do not gain.
         [&](int m, int n, const u32x4& v) {
           if (m0 + m < a.M && n0 + n < a.N) {
-            *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.dw) + base + int64_t(m) * a.N + n) =
-                v;
+            __builtin_nontemporal_store(
+                v, reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.dw) + base + int64_t(m) * a.N + n));
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               square(low(v[k]));
@@ -141,7 +170,8 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
           if constexpr (kEarly) was = old[q];
           if constexpr (kF32) {
             if constexpr (kAcc) v += was;
-            *p = v;
+            if constexpr (kAcc) *p = v;
+            else __builtin_nontemporal_store(v, p);
           } else {
             const u32x2 r{pack(v[0] + low(was.x), v[1] + high(was.x)),
                           pack(v[2] + low(was.y), v[3] + high(was.y))};
@@ -170,6 +200,7 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
 
 template <bool kDgrad>
 void launch_rows(GroupedRows a, hipStream_t s) {
+  a.past = past_caches(a.g.rows, a.N);
   auto launch = [&](auto edge, auto share, int64_t wgs) {
     hipLaunchKernelGGL((k6_rows<kDgrad, decltype(edge)::value, decltype(share)::value>),
                        dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
@@ -184,7 +215,7 @@ void launch_wgrad_of(GroupedWgrad a, hipStream_t s) {
     a.tiles_m = (a.M + kT - 1) / kT;
     a.tiles_n = (a.N + kT - 1) / kT;
     hipLaunchKernelGGL((k6_wgrad<kF32, kAcc, kT>),
-                       dim3(unsigned(int64_t(a.g.num) * a.tiles_m * a.tiles_n)),
+                       dim3(unsigned(int64_t(a.g.num) * slots_of(a.g.num, a.tiles_m * a.tiles_n))),
                        dim3(mm::kThreads), 0, s, a);
   };
   // 256 tiles where experts have rows enough to outweigh what a tile takes beside its

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, false, kT>::kPerCu)
       },
       [&](int m, int n, const u32x4& v) {
         if (m < t.rows && n0 + n < a.N)
-          *reinterpret_cast<u32x4*>(a.y + int64_t(t.row + m) * a.y_stride + n0 + n) = v;
+          put(reinterpret_cast<u32x4*>(a.y + int64_t(t.row + m) * a.y_stride + n0 + n), v, a.past);
       });
 }
 
@@ -264,6 +264,7 @@ hipError_t launch_quantized_token(const QuantizedToken& a, hipStream_t s) {
 }
 
 hipError_t launch_quantized_linear(QuantizedLinear a, hipStream_t s) {
+  a.past = past_caches(a.g.rows, a.N);
   auto launch = [&](auto edge, auto share, int64_t wgs) {
     hipLaunchKernelGGL((k7_linear<decltype(edge)::value, decltype(share)::value>),
                        dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
