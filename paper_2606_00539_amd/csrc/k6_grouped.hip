@@ -143,7 +143,8 @@ __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) 
         // Gradients that nothing was added to go past the caches: what they would drive out is dy and
         // x.  64 and 24 experts 2048 x 1408 of 384 rows, us through and past them: fp32 313 and 201, 110
         // and 74, bf16 227 and 163, 67 and 65; with a pass that reads the gradient behind it fp32 554
-        // and 522.  (Where experts have a row or two, 13% slower.)  Accumulated ones do not gain.
+        // and 522.  (Experts of a row or two are up to 13%
+        // slower so.)  Accumulated ones do not gain.
         [&](int m, int n, const u32x4& v) {
           if (m0 + m < a.M && n0 + n < a.N) {
             __builtin_nontemporal_store(
