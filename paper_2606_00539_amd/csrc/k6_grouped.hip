@@ -62,7 +62,7 @@ __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, kDgrad, kT>::kPerCu
 
 // The 128 tile's three stages leave room for three workgroups on a CU; where it holds fp32 values
 // to add to, their registers allow two, and there is room for four stages.  64 experts 2048 x
-// 1408, 24,576 rows, three and two on a CU: bf16 269 and 289 us, accumulating 319 and 347, fp32
+// 1408, 24,576 rows, three and two on a CU (all through the caches): bf16 269 and 289 us, accumulating 319 and 347, fp32
 // 334 and 365, accumulating 536 and 431.
 template <bool kF32, bool kAcc, int kT>
 struct WgradTile {
@@ -220,7 +220,8 @@ void launch_wgrad_of(GroupedWgrad a, hipStream_t s) {
                        dim3(mm::kThreads), 0, s, a);
   };
   // 256 tiles where experts have rows enough to outweigh what a tile takes beside its
-  // steps, and tiles enough for the chip.  us in 128 and 256 tiles, bf16 and accumulating: 64
+  // steps, and tiles enough for the chip.  us in 128 and 256 tiles, bf16 and accumulating (all
+  // through the caches; past them the first are 178, 714 and 931 as chosen): 64
   // experts 2048 x 1408 of 384 rows 269 and 282, 319 and 621; 8 of 4096 x 11008 of 1,024
   // rows 861 and 855, 980 and 1,543; one of 5120 x 13824 of 8,192 rows 1,524 and 951, 1,483 and
   // 1,096; one of 4096 x 4096 of 4,096 rows 130 and 109, 142 and 133.
