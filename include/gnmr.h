@@ -469,7 +469,8 @@ gnmr_status gnmr_quantized_linear(const gnmr_groups* groups, const void* x, int6
  * in, out: device [count][rows][cols], contiguous, in of in_dtype (GNMR_BF16 or GNMR_F32), out
  * bf16.  rows, cols 1 .. 65536 (any parity); the products run on the matrix cores in fp16 with
  * scaled iterates and fp32 accumulation, which holds them to about 2^-11 relative each.
- * The coefficients have to keep the singular values below 16.  G = 0 gives 0; a G with an
+ * The coefficients have to keep the singular values of X below 15.9 at the start of every step
+ * (they start in [0, 1]); a + b s + c s^2 may take any value that fp32 holds.  G = 0 gives 0; a G with an
  * infinity or a NaN gives NaN throughout.  workspace: device, 256-byte aligned, of at least
  * gnmr_orthogonalize_workspace(rows, cols, count) bytes. */
 typedef struct {

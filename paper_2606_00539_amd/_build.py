@@ -15,7 +15,7 @@ SOURCES = [os.path.join(PKG, "csrc", f)
                      "k7_quantized.hip", "k8_orthogonal.hip")]
 HEADERS = [os.path.join(PKG, "csrc", f)
            for f in ("gnmr_internal.h", "groups.h", "host_call.h", "k1_geometry.h", "k1_item.h",
-                     "k3_pool.h", "lane_ops.h", "launch_tag.h", "mm_tile.h", "unit_step.h")] + [os.path.join(ROOT, "include", "gnmr.h")]
+                     "k3_pool.h", "k8_range.h", "lane_ops.h", "launch_tag.h", "mm_tile.h", "unit_step.h")] + [os.path.join(ROOT, "include", "gnmr.h")]
 
 # Marshalling of the per-step calls (host code), for the Python that builds it: the
 # name carries that Python's ABI, so that no other one loads it.

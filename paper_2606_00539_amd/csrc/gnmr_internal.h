@@ -230,6 +230,7 @@ struct Orthogonal {
   __bf16* out;            // [count][rows][cols]
   int32_t rows, cols, count;
   float ca, cb, cc, eps, scale;
+  float held_a, held_p;   // what A and P are multiplied by in fp16 (powers of two)
   bool f32;
   // set by launch_orthogonal
   bool flip, first;       // flip: X is the transpose of the update

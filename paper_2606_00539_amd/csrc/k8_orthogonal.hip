@@ -7,10 +7,13 @@
 //
 // drives every singular value of G towards 1 and keeps its singular vectors.
 //
-// The iterates are held in fp16 between the products, scaled by 2^12: |X| <= its
-// largest singular value, which the usual coefficients keep below 1.3 (and |P| below
-// 4), so the range holds values from 2^-26 (with all 11 bits) to 16, and each product's
-// rounding is 2^-12 relative, an eighth of bf16's at the same matrix-core rate.  Products
+// The iterates are held in fp16 between the products, X scaled by 2^12: |X| <= its
+// largest singular value, so the range holds values from 2^-26 (with all 11 bits) to 15.99, and each
+// product's rounding is 2^-12 relative, an eighth of bf16's at the same matrix-core rate.  |A| can
+// reach the square of that value and |P| what the polynomial makes of it: their powers of two follow
+// from the coefficients (k8_range.h), 2^12 too with the usual ones, whose |A| stays below 1.5
+// and |P| below 4.  With lower ones their small values lose bits, but A and P act as wholes: what
+// counts is the rounding beside their largest.  Products
 // accumulate in fp32.  a is part of P's diagonal and is rounded with it, to 2^-12
 // of at most a: as much again as X's own rounding, and less than the error of the
 // result in bf16; added to the product in fp32 it would cost a read of X for every
@@ -19,6 +22,7 @@
 // first iteration's factors.  The norm is summed in float64.
 #include "gnmr_internal.h"
 #include "groups.h"
+#include "k8_range.h"
 #include "lane_ops.h"
 #include "mm_tile.h"
 
@@ -40,8 +44,9 @@ __device__ __forceinline__ u32x2 half4(float a, float b, float c, float d) {
   return __builtin_bit_cast(u32x2, f16x4{_Float16(a), _Float16(b), _Float16(c), _Float16(d)});
 }
 
-constexpr float kHeld = 0x1p12f;       // what X, A and P are multiplied by in fp16
+constexpr float kHeld = 0x1p12f;       // what X is multiplied by in fp16
 constexpr float kUnheld = 0x1p-12f;
+static_assert(kHeld == float(1 << kHeldX), "X is held as its range assumes");
 
 // Eight values from p, which is aligned to 16 bytes.
 template <bool kF32>
@@ -216,7 +221,9 @@ __global__ __launch_bounds__(
   const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * what is held
   if constexpr (!kIntoX) {
     _Float16* to = kWhat == kGram ? A : P;
-    const float s = f * f * kHeld, p = a.cb, q = a.cc * kUnheld, one = a.ca * kHeld;
+    // (1 / held_a is a power of two, as held_p is)
+    const float s = f * f * a.held_a, per_a = a.held_p / a.held_a;
+    const float p = a.cb * per_a, q = a.cc * (per_a / a.held_a), one = a.ca * a.held_p;
     T::change(acc, wave, lane, [&](int e, int m, int n, f32x4 c) {
       if constexpr (kWhat == kGram) return c * s;
       f16x4 h;
@@ -242,10 +249,11 @@ __global__ __launch_bounds__(
     });
   } else if constexpr (kWhat == kApply) {
     _Float16* to = a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np;
+    const float s = f * (kHeld / a.held_p);
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
-          return half4(f * a0, f * a1, f * a2, f * a3);
+          return half4(s * a0, s * a1, s * a2, s * a3);
         },
         [&](int m, int n, const u32x4& h) {
           if (m0 + m < a.mp && n0 + n < a.np)
@@ -257,7 +265,7 @@ __global__ __launch_bounds__(
     const int row0 = kFlip ? n0 : m0, col0 = kFlip ? m0 : n0;
     __bf16* out = a.out + int64_t(mat) * a.m * a.n;
     const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-    const float s = kUnheld * (f * a.scale);
+    const float s = (f * a.scale) / a.held_p;
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
@@ -354,6 +362,9 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   a.n = a.flip ? a.rows : a.cols;
   a.mp = pad(a.m);
   a.np = pad(a.n);
+  const HeldExponents held = held_exponents(a.ca, a.cb, a.cc, steps);
+  a.held_a = ldexpf(1.0f, held.a);
+  a.held_p = ldexpf(1.0f, held.p);
   char* w = static_cast<char*>(workspace);
   a.sums = reinterpret_cast<double*>(w);
   a.parts = norm_parts(int64_t(a.rows) * a.cols, a.count);
