@@ -236,8 +236,10 @@ struct Orthogonal {
   bool flip, first;       // flip: X is the transpose of the update
   int32_t m, n, mp, np, now, tiles_m, tiles_n, tiles, first_tile, num_tiles;
   int32_t parts;
+  int32_t growth, spent;  // what a step takes off `extra`, and the steps before have taken
   double* sums;           // [count][parts], partial sums of squares
-  float* factor;          // [count], first iteration: X = factor * what is held
+  float* factor;          // [count], first iteration: X = factor * 2^-extra * what is held
+  int32_t* extra;         // [count], powers of two that X is held higher by at first
   _Float16* x[2];         // [count][mp][np]
   _Float16 *A, *P;        // [count][mp][mp]
 };

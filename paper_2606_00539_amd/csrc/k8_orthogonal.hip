@@ -20,6 +20,8 @@
 // product (64 updates of 1408 x 2048: 640 us a product, 540 without).  The first X is
 // G times a power of two, exact for bf16 input; what is left of the norm goes into the
 // first iteration's factors.  The norm is summed in float64.
+// Where eps is larger than the norm, X starts that much below 1 and is held as many powers of two
+// higher, fewer by every step by what it may grow: it keeps its bits however small.
 #include "gnmr_internal.h"
 #include "groups.h"
 #include "k8_range.h"
@@ -117,12 +119,19 @@ __global__ __launch_bounds__(256) void k8_load(const Orthogonal a) {
   ss = wave_sum(ss);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
   __syncthreads();
-  const double norm = sqrt(((red[0] + red[1]) + red[2]) + red[3]) + double(a.eps);
-  int k = 0;
+  const double length = sqrt(((red[0] + red[1]) + red[2]) + red[3]);
+  const double norm = length + double(a.eps);
+  int k = 0, extra = 0;
   (void)frexp(norm, &k);            // norm = f * 2^k, f in [0.5, 1)
-  const int up = 12 - k;            // |G| * 2^up <= 2^12
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-    a.factor[mat] = norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, up));
+  if (length > 0.0 && length < norm) {
+    (void)frexp(norm / length, &extra);
+    --extra;                        // length * 2^extra <= norm (0 where length is infinite)
+  }
+  const int up = 12 - k + extra;    // |G| * 2^up <= 2^12
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    a.factor[mat] = norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, 12 - k));
+    a.extra[mat] = extra;
+  }
   // eight consecutive elements of a row of G to a lane: rows r0 .. r0+63 from column c0
   const char* in = static_cast<const char*>(a.in) + int64_t(mat) * size * kSize;
   const int r0 = kFlip ? n0 : m0, c0 = kFlip ? m0 : n0;
@@ -217,17 +226,18 @@ __global__ __launch_bounds__(
   f16x4 old[kEarly ? T::kGroups : 1];
   if constexpr (kEarly)
     T::groups(wave, lane, [&](int e, int m, int n) { old[e] = stored(m, n); });
+  const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * 2^-e * what is held
+  const int extra = a.extra[mat], e = max(extra - a.spent, 0);
   T::product(acc, om, on, K, wave, lane);
-  const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * what is held
   if constexpr (!kIntoX) {
     _Float16* to = kWhat == kGram ? A : P;
     // (1 / held_a is a power of two, as held_p is)
-    const float s = f * f * a.held_a, per_a = a.held_p / a.held_a;
+    const float s = ldexpf(f * f * a.held_a, -2 * e), per_a = a.held_p / a.held_a;
     const float p = a.cb * per_a, q = a.cc * (per_a / a.held_a), one = a.ca * a.held_p;
-    T::change(acc, wave, lane, [&](int e, int m, int n, f32x4 c) {
+    T::change(acc, wave, lane, [&](int group, int m, int n, f32x4 c) {
       if constexpr (kWhat == kGram) return c * s;
       f16x4 h;
-      if constexpr (kEarly) h = old[e];
+      if constexpr (kEarly) h = old[group];
       else h = stored(m, n);
       f32x4 r;
 #pragma unroll
@@ -249,7 +259,7 @@ __global__ __launch_bounds__(
     });
   } else if constexpr (kWhat == kApply) {
     _Float16* to = a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np;
-    const float s = f * (kHeld / a.held_p);
+    const float s = ldexpf(f * (kHeld / a.held_p), max(extra - a.spent - a.growth, 0) - e);
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
@@ -265,7 +275,7 @@ __global__ __launch_bounds__(
     const int row0 = kFlip ? n0 : m0, col0 = kFlip ? m0 : n0;
     __bf16* out = a.out + int64_t(mat) * a.m * a.n;
     const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-    const float s = (f * a.scale) / a.held_p;
+    const float s = ldexpf((f * a.scale) / a.held_p, -e);
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
@@ -353,7 +363,7 @@ int norm_parts(int64_t size, int count) {
 int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count) {
   const int64_t mp = pad(std::min(rows, cols)), np = pad(std::max(rows, cols));
   return up256(int64_t(count) * norm_parts(int64_t(rows) * cols, count) * 8) +
-         up256(int64_t(count) * 4) + int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
+         2 * up256(int64_t(count) * 4) + int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
 }
 
 hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream_t s) {
@@ -365,11 +375,14 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   const HeldExponents held = held_exponents(a.ca, a.cb, a.cc, steps);
   a.held_a = ldexpf(1.0f, held.a);
   a.held_p = ldexpf(1.0f, held.p);
+  a.growth = held.growth;
   char* w = static_cast<char*>(workspace);
   a.sums = reinterpret_cast<double*>(w);
   a.parts = norm_parts(int64_t(a.rows) * a.cols, a.count);
   w += up256(int64_t(a.count) * a.parts * 8);
   a.factor = reinterpret_cast<float*>(w);
+  w += up256(int64_t(a.count) * 4);
+  a.extra = reinterpret_cast<int32_t*>(w);
   w += up256(int64_t(a.count) * 4);
   const int64_t xs = int64_t(a.count) * a.mp * a.np, as = int64_t(a.count) * a.mp * a.mp;
   a.x[0] = reinterpret_cast<_Float16*>(w);
@@ -387,6 +400,7 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   for (int i = 0; i < steps; ++i) {
     a.first = i == 0;
     a.now = i & 1;
+    a.spent = i * a.growth;
     launch_product<kGram, false>(a, s);
     launch_product<kPoly, false>(a, s);
     if (i + 1 < steps) launch_product<kApply, false>(a, s);

@@ -42,7 +42,8 @@ struct StepPolynomial {
 };
 
 struct HeldExponents {
-  int a, p;   // A is held times 2^a, P times 2^p
+  int a, p;     // A is held times 2^a, P times 2^p
+  int growth;   // a step multiplies no singular value by more than 2^growth
 };
 
 // An update starts with singular values in [0, 1], since its Frobenius norm is at most 1.  Each
@@ -62,7 +63,8 @@ inline HeldExponents held_exponents(float a, float b, float c, int steps) {
     const double e = floor(log2(kMostHalf / (kSlack * std::max(most, 1e-30))));
     return int(std::max(-120.0, std::min(double(kHeldX), e)));
   };
-  return HeldExponents{exponent(most_a), exponent(most_p)};
+  const int growth = most_p > 0.0 ? int(std::max(0.0, ceil(log2(kSlack * most_p)))) : 0;
+  return HeldExponents{exponent(most_a), exponent(most_p), growth};
 }
 
 }  // namespace gnmr

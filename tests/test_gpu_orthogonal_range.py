@@ -1,5 +1,5 @@
 """K8 with coefficients that take A = X X^T and the polynomial past what fp16 holds at the
-usual scale, against the formulas in float64.
+usual scale, and updates whose norm lies far below eps, against the formulas in float64.
 
 Tolerance.  The updates have rows that are orthogonal and equally long (one row, or some of
 a Hadamard matrix), so that A = s I and every step multiplies X by p(s): with u = 2^-11
@@ -69,4 +69,27 @@ def test_large_coefficients(coefficients, steps, shape):
     g, want = (g, want) if shape[0] <= shape[1] else (g.T.copy(), want.T)
     got = run(g, coefficients, steps, 0.0)
     assert np.isfinite(got).all()
+    assert np.abs(got - want).max() <= limit * np.abs(want).max(), limit
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 300), (300, 1), (64, 128), (256, 64)])
+@pytest.mark.parametrize("length,eps,steps", [
+    (1e-3, 1e-4, 1), (1e-7, 1e-7, 1), (1e-9, 1e-7, 1), (1e-30, 1.0, 1), (1e-13, 1e-7, 5),
+    (1e-25, 1e-7, 5), (1e-30, 1.0, 5), (1e-36, 1e-3, 5)])
+def test_norm_below_eps(length, eps, shape, steps, dtype):
+    """X = G / (|G| + eps) is small then, and grows by a = 3.4445 a step."""
+    torch = require_gpu()
+    m, n = min(shape), max(shape)
+    g = updates(m, n)
+    g = (g * (length / np.linalg.norm(g))).astype(np.float32)
+    if dtype == "bf16":
+        g = X.bf16(g)
+    coefficients = (3.4445, -4.775, 2.0315)
+    want = X.orthogonalize(g, steps, coefficients, float(np.float32(eps)))
+    s = (np.linalg.norm(g.astype(np.float64)) / (np.linalg.norm(g.astype(np.float64)) + eps)) ** 2
+    limit = bound(s / m, coefficients, steps)
+    g, want = (g, want) if shape[0] <= shape[1] else (g.T.copy(), want.T)
+    got = run(g, coefficients, steps, eps, torch.bfloat16 if dtype == "bf16" else None)
+    assert np.abs(want).max() > 1e-37
     assert np.abs(got - want).max() <= limit * np.abs(want).max(), limit
