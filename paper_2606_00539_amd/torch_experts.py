@@ -24,6 +24,19 @@ def _readable(dy):
     return dy.clone(memory_format=torch.contiguous_format)
 
 
+class _FirstDerivative(torch.autograd.Function):
+    """dx where backward is itself recorded: it depends on `dy` and `weight`, and whoever asks how
+    is refused (the kernels that made it are not recorded)."""
+
+    @staticmethod
+    def forward(ctx, dx, dy, weight):
+        return dx.view_as(dx)
+
+    @staticmethod
+    def backward(ctx, g):
+        raise RuntimeError("ExpertUnits.linear has no second derivatives")
+
+
 class _ExpertLinear(torch.autograd.Function):
     """y[t] = W_e x[t]: in bf16 for the experts of A_t, in INT8 for the others.  Backward
     takes the products with the bf16 weights and the bf16 input on both paths (a
@@ -44,10 +57,12 @@ class _ExpertLinear(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, weight, offsets = ctx.saved_tensors
-        dy = _readable(dy)
-        dx = ops.grouped_dgrad(dy, weight, offsets) if ctx.needs_input_grad[0] else None
+        rows = _readable(dy.detach())
+        dx = ops.grouped_dgrad(rows, weight, offsets) if ctx.needs_input_grad[0] else None
         if ctx.needs_input_grad[1]:
-            ctx.units._weight_grad(ctx.k, dy, x, offsets)
+            ctx.units._weight_grad(ctx.k, rows, x, offsets)
+        if dx is not None and torch.is_grad_enabled():      # create_graph
+            dx = _FirstDerivative.apply(dx, dy, weight)
         return dx, None, None, None, None
 
 
@@ -63,7 +78,8 @@ class ExpertUnits:
 
     Backward writes the weight gradients itself, into `grads[name]` in grad_dtype,
     adding over the micro-batches since the last `step()`, and the sums of squares of
-    what it stores; `step()` runs the controller from those.  weight.grad stays None.
+    what it stores; `step()` runs the controller from those.  weight.grad stays None.  Second
+    derivatives are refused.
     """
 
     def __init__(self, named_weights, window: int = 5, max_o: int = 8, lock_len: int = 8,
