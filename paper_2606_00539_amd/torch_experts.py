@@ -37,15 +37,43 @@ class _FirstDerivative(torch.autograd.Function):
         raise RuntimeError("ExpertUnits.linear has no second derivatives")
 
 
+class _Use:
+    """One use of matrix k in a product: what its weight gradient is formed from, between the
+    backward of the product and that of the weight."""
+
+    def __init__(self, units, k):
+        self.units, self.k, self.rows = units, k, None
+
+    def write(self):
+        rows, self.rows = self.rows, None
+        self.units._weight_grad(self.k, *rows)
+
+
+class _WeightUse(torch.autograd.Function):
+    """An empty tensor between the weight and its product: autograd comes here only where a
+    weight gradient is asked for, which the product itself cannot see."""
+
+    @staticmethod
+    def forward(ctx, weight, use):
+        ctx.use = use
+        return weight.new_empty(0)
+
+    @staticmethod
+    def backward(ctx, _):
+        ctx.use.write()
+        return None, None
+
+
 class _ExpertLinear(torch.autograd.Function):
     """y[t] = W_e x[t]: in bf16 for the experts of A_t, in INT8 for the others.  Backward
     takes the products with the bf16 weights and the bf16 input on both paths (a
     straight-through gradient)."""
 
     @staticmethod
-    def forward(ctx, x, weight, offsets, units, k):
+    def forward(ctx, x, weight, token, offsets, use):
         ctx.save_for_backward(x, weight, offsets)
-        ctx.units, ctx.k = units, k
+        ctx.use = use
+        units, k = use.units, use.k
         if units.codes[k] is None:
             return ops.grouped_linear(x, weight, offsets)
         y = torch.empty(x.shape[0], weight.shape[1], dtype=x.dtype, device=x.device)
@@ -57,13 +85,13 @@ class _ExpertLinear(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, weight, offsets = ctx.saved_tensors
-        rows = _readable(dy.detach())
+        rows, token = _readable(dy.detach()), None
         dx = ops.grouped_dgrad(rows, weight, offsets) if ctx.needs_input_grad[0] else None
-        if ctx.needs_input_grad[1]:
-            ctx.units._weight_grad(ctx.k, rows, x, offsets)
+        if ctx.needs_input_grad[2]:
+            ctx.use.rows, token = (rows, x, offsets), rows.new_empty(0)
         if dx is not None and torch.is_grad_enabled():      # create_graph
             dx = _FirstDerivative.apply(dx, dy, weight)
-        return dx, None, None, None, None
+        return dx, None, token, None, None
 
 
 class ExpertUnits:
@@ -76,7 +104,8 @@ class ExpertUnits:
     made by `refresh()`, which an optimiser calls after it has changed them); the
     controller's mask is read on the device when the kernels run.
 
-    Backward writes the weight gradients itself, into `grads[name]` in grad_dtype,
+    Backward writes the weight gradients itself, into `grads[name]` in grad_dtype, where it is
+    asked for them (`torch.autograd.grad(loss, x)` leaves them alone),
     adding over the micro-batches since the last `step()`, and the sums of squares of
     what it stores; `step()` runs the controller from those.  weight.grad stays None.  Second
     derivatives are refused.
@@ -137,7 +166,8 @@ class ExpertUnits:
 
     def linear(self, name, x, offsets):
         k = self._index[name]
-        return _ExpertLinear.apply(x, self.weights[k], offsets, self, k)
+        use, weight = _Use(self, k), self.weights[k]
+        return _ExpertLinear.apply(x, weight, _WeightUse.apply(weight, use), offsets, use)
 
     def _weight_grad(self, k, dy, x, offsets):
         E = self.weights[k].shape[0]
