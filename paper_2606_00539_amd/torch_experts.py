@@ -106,7 +106,7 @@ class ExpertUnits:
 
     Backward writes the weight gradients itself, into `grads[name]` in grad_dtype, where it is
     asked for them (`torch.autograd.grad(loss, x)` leaves them alone),
-    adding over the micro-batches since the last `step()`, and the sums of squares of
+    adding over the micro-batches since the last `step()` (or `zero_grad()`), and the sums of squares of
     what it stores; `step()` runs the controller from those.  weight.grad stays None.  Second
     derivatives are refused.
     """
@@ -139,6 +139,7 @@ class ExpertUnits:
         self.grads = {n: torch.empty(w.shape, dtype=grad_dtype, device=device)
                       for n, w in zip(self.names, self.weights)}
         self._filled = [False] * len(self.weights)
+        self._started = [0] * len(self.weights)     # gradients started, by matrix
         U = first[-1]
         off = np.zeros(U + 1, np.int64)
         for k, w in enumerate(self.weights):
@@ -174,7 +175,12 @@ class ExpertUnits:
         ops.grouped_wgrad(dy, x, offsets, dw=self.grads[self.names[k]],
                           accumulate=self._filled[k],
                           partials=self.partials[self._parts[k]:self._parts[k + 1]].view(E, -1))
+        self._started[k] += not self._filled[k]
         self._filled[k] = True
+
+    def zero_grad(self) -> None:
+        """The next backward starts the gradients anew, without a controller step."""
+        self._filled = [False] * len(self.weights)
 
     def step(self, alpha_t: float, beta_t: float, stream=None) -> None:
         """One controller step from the gradients since the last one (asynchronous)."""
@@ -211,7 +217,9 @@ class _DeviceBytes:
 class OrthogonalMomentum:
     """Updates the weights of ExpertUnits with their orthogonalised momentum: per matrix
     m = momentum * m + g (fp32), W -= lr * max(1, out / in)^0.5 * orthogonalize(m), all
-    experts of a matrix in one call; then the units' codes are made again."""
+    experts of a matrix in one call; then the units' codes are made again.  Each gradient is
+    taken once: `units.step()` or `units.zero_grad()` comes between an update and the next
+    backward, else that would add to what was applied, and `step()` raises."""
 
     def __init__(self, units, lr: float, momentum: float = 0.95, steps: int = 5,
                  coefficients=ops.COEFFICIENTS, eps: float = 1e-7):
@@ -219,9 +227,14 @@ class OrthogonalMomentum:
         self.steps, self.coefficients, self.eps = steps, coefficients, eps
         self.buffers = {n: torch.zeros(g.shape, dtype=torch.float32, device=g.device)
                         for n, g in units.grads.items()}
+        self._applied = [0] * len(units.weights)    # units._started of the last update
 
     @torch.no_grad()
     def step(self) -> None:
+        for name, started, applied in zip(self.units.names, self.units._started, self._applied):
+            if started == applied:
+                raise RuntimeError(f"{name}: no gradient was started since the last update")
+        self._applied = list(self.units._started)
         for name, w in zip(self.units.names, self.units.weights):
             m = self.buffers[name]
             m.mul_(self.momentum).add_(self.units.grads[name])

@@ -64,11 +64,15 @@ def grouped_wgrad(dy, x, offsets, dw, accumulate=False, partials=None):
     return dw, partials
 
 
+def orthogonalize(x, steps=5, coefficients=None, eps=1e-7, scale=1.0):
+    return (scale * torch.sign(x)).to(torch.bfloat16)
+
+
 def patch(monkeypatch):
     """Puts the plain forms in place of what needs a device."""
     monkeypatch.setattr(E, "Controller", NotedController)
     monkeypatch.setattr(E, "_DeviceBytes", lambda ctl, n: np.zeros(n, np.uint8))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: ("stream of", device))
     monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
-    for f in (grouped_linear, grouped_dgrad, grouped_wgrad):
+    for f in (grouped_linear, grouped_dgrad, grouped_wgrad, orthogonalize):
         monkeypatch.setattr(E.ops, f.__name__, f)
