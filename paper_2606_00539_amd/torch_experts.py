@@ -12,7 +12,6 @@ import torch
 
 from . import torch_ops as ops
 from .binding import GNMR_BUDGET_ACTIVE, Controller, gnmr_grouped_wgrad_num_partials
-from .torch_units import _current
 
 
 def _readable(dy):
@@ -120,6 +119,9 @@ class ExpertUnits:
             if w.dim() != 3 or w.dtype != torch.bfloat16 or not w.is_cuda or not w.is_contiguous():
                 raise TypeError(f"{name}: the weight must be a contiguous bf16 [experts, out, in] "
                                 "tensor on a HIP device")
+            if self.weights and w.device != self.weights[0].device:
+                raise ValueError(f"{name}: all weights must be on one device, {w.device} is not "
+                                 f"{self.weights[0].device}")
             E, o, i = w.shape
             if o % 8 or i % 8:
                 raise ValueError(f"{name}: features must be multiples of 8, got {o}x{i}")
@@ -134,7 +136,7 @@ class ExpertUnits:
             raise TypeError("grad_dtype must be torch.bfloat16 or torch.float32")
         self._index = {n: k for k, n in enumerate(self.names)}
         self._first, self._parts = first, parts
-        device = self.weights[0].device
+        device = self.device = self.weights[0].device
         self.partials = torch.zeros(parts[-1], dtype=torch.float32, device=device)
         self.grads = {n: torch.empty(w.shape, dtype=grad_dtype, device=device)
                       for n, w in zip(self.names, self.weights)}
@@ -148,13 +150,18 @@ class ExpertUnits:
         rec = None
         if recoverable is not None:
             rec = np.array([1 if recoverable(u) else 0 for u in self.unit_names], np.uint8)
-        self.ctl = Controller(U, window, max_o, lock_len, eps, np.zeros(U + 1, np.int64), [], [],
-                              None, rec, _current(stream), budget_mode, warmup_steps)
+        with torch.cuda.device(device):         # a controller is the current device's
+            self.ctl = Controller(U, window, max_o, lock_len, eps, np.zeros(U + 1, np.int64), [],
+                                  [], None, rec, self._stream(stream), budget_mode, warmup_steps)
         self.ctl.bind_partials(off)
         self._mask = torch.as_tensor(_DeviceBytes(self.ctl, U), device=device)
         self.low_cost = bool(low_cost)
         self.codes = [None] * len(self.weights)
         self.refresh()
+
+    def _stream(self, stream):
+        """`stream`, or torch's current one on the weights' device when it is None."""
+        return torch.cuda.current_stream(self.device) if stream is None else stream
 
     def mask(self, k):
         """The controller's mask over matrix k's experts (device memory of the controller)."""
@@ -187,16 +194,16 @@ class ExpertUnits:
         for n, done in zip(self.names, self._filled):
             if not done:
                 raise RuntimeError(f"{n}: no gradient was written since the last step")
-        self.ctl.step_from_partials(self.partials, alpha_t, beta_t, _current(stream))
+        self.ctl.step_from_partials(self.partials, alpha_t, beta_t, self._stream(stream))
         self._filled = [False] * len(self.weights)
 
     def query(self, stream=None) -> dict:
-        out = self.ctl.query(_current(stream))
+        out = self.ctl.query(self._stream(stream))
         out["units"] = self.unit_names
         return out
 
     def recovery_set(self, stream=None) -> list:
-        m = self.ctl.query(_current(stream))["mask"]
+        m = self.ctl.query(self._stream(stream))["mask"]
         return [u for u, a in zip(self.unit_names, m) if a]
 
     def close(self):
