@@ -168,9 +168,11 @@ class ExpertUnits:
         return self._mask[self._first[k]:self._first[k + 1]]
 
     def refresh(self) -> None:
-        """The weights' INT8 codes again, after the weights have changed."""
+        """The weights' INT8 codes again, after the weights have changed.  They stay where they
+        are, for captured graphs and for what another stream is still reading."""
         if self.low_cost:
-            self.codes = [ops.quantize_rows(w.detach()) for w in self.weights]
+            self.codes = [ops.quantize_rows(w.detach(), out=c)
+                          for w, c in zip(self.weights, self.codes)]
 
     def linear(self, name, x, offsets):
         k = self._index[name]

@@ -172,15 +172,24 @@ def grouped_wgrad(dy, x, offsets=None, mask=None, mask_value=1, dw=None, accumul
     return dw, partials
 
 
-def quantize_rows(x):
+def quantize_rows(x, out=None):
     """(codes, scale): symmetric INT8 codes of x's rows (over its last dimension; any
-    leading ones) and the fp32 scale of each."""
+    leading ones) and the fp32 scale of each; `out` is such a pair to write them to."""
     if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 2:
         raise TypeError("x must be a bf16 or fp32 tensor of rows on a HIP device")
     flat = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
     _matrix("x", flat, x.dtype)
-    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    if out is None:
+        codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+        scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    else:
+        codes, scale = out
+        for name, t, shape, dtype in (("codes", codes, x.shape, torch.int8),
+                                      ("scale", scale, x.shape[:-1], torch.float32)):
+            if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+                raise TypeError(f"{name} must be a contiguous {dtype} tensor of shape "
+                                f"{tuple(shape)}")
+        _same_device(x, codes, scale)
     device, stream = _on(x)
     with device:
         B.gnmr_quantize_rows(flat, _DTYPES[x.dtype], _stride(flat), codes, scale, flat.shape[0],
