@@ -23,6 +23,10 @@ def _readable(dy):
     return dy.clone(memory_format=torch.contiguous_format)
 
 
+def _handle(stream):
+    return int(getattr(stream, "cuda_stream", stream))
+
+
 class _FirstDerivative(torch.autograd.Function):
     """dx where backward is itself recorded: it depends on `dy` and `weight`, and whoever asks how
     is refused (the kernels that made it are not recorded)."""
@@ -142,6 +146,7 @@ class ExpertUnits:
                       for n, w in zip(self.names, self.weights)}
         self._filled = [False] * len(self.weights)
         self._started = [0] * len(self.weights)     # gradients started, by matrix
+        self._writers = [None] * len(self.weights)  # the stream that last wrote each
         U = first[-1]
         off = np.zeros(U + 1, np.int64)
         for k, w in enumerate(self.weights):
@@ -179,11 +184,22 @@ class ExpertUnits:
         use, weight = _Use(self, k), self.weights[k]
         return _ExpertLinear.apply(x, weight, _WeightUse.apply(weight, use), offsets, use)
 
+    def _after_writers(self, stream, writers):
+        """Work that follows on `stream` runs after the gradients' writers.  (Backward runs where
+        forward did, on several streams perhaps; autograd orders only what passes through it.)"""
+        for w in {_handle(w): w for w in writers if w is not None}.values():
+            if _handle(w) != _handle(stream):
+                if not hasattr(stream, "wait_stream"):
+                    stream = torch.cuda.ExternalStream(_handle(stream), device=self.device)
+                stream.wait_stream(w)
+
     def _weight_grad(self, k, dy, x, offsets):
-        E = self.weights[k].shape[0]
+        E, stream = self.weights[k].shape[0], self._stream(None)
+        self._after_writers(stream, self._writers[k:k + 1])
         ops.grouped_wgrad(dy, x, offsets, dw=self.grads[self.names[k]],
                           accumulate=self._filled[k],
                           partials=self.partials[self._parts[k]:self._parts[k + 1]].view(E, -1))
+        self._writers[k] = stream
         self._started[k] += not self._filled[k]
         self._filled[k] = True
 
@@ -196,7 +212,9 @@ class ExpertUnits:
         for n, done in zip(self.names, self._filled):
             if not done:
                 raise RuntimeError(f"{n}: no gradient was written since the last step")
-        self.ctl.step_from_partials(self.partials, alpha_t, beta_t, self._stream(stream))
+        stream = self._stream(stream)
+        self._after_writers(stream, self._writers)
+        self.ctl.step_from_partials(self.partials, alpha_t, beta_t, stream)
         self._filled = [False] * len(self.weights)
 
     def query(self, stream=None) -> dict:
@@ -244,6 +262,7 @@ class OrthogonalMomentum:
             if started == applied:
                 raise RuntimeError(f"{name}: no gradient was started since the last update")
         self._applied = list(self.units._started)
+        self.units._after_writers(self.units._stream(None), self.units._writers)
         for name, w in zip(self.units.names, self.units.weights):
             m = self.buffers[name]
             m.mul_(self.momentum).add_(self.units.grads[name])

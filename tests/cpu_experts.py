@@ -20,6 +20,11 @@ def weight(*shape, seed=0):
     return w.as_subclass(OnDevice).requires_grad_()
 
 
+class TheStream:
+    """The one stream there is."""
+    cuda_stream = 0
+
+
 class NotedController:
     def __init__(self, *args):
         self.calls = [("init",) + args]
@@ -72,7 +77,7 @@ def patch(monkeypatch):
     """Puts the plain forms in place of what needs a device."""
     monkeypatch.setattr(E, "Controller", NotedController)
     monkeypatch.setattr(E, "_DeviceBytes", lambda ctl, n: np.zeros(n, np.uint8))
-    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: ("stream of", device))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: TheStream)
     monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
     for f in (grouped_linear, grouped_dgrad, grouped_wgrad, orthogonalize):
         monkeypatch.setattr(E.ops, f.__name__, f)
