@@ -73,6 +73,12 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 
+// Between what lanes of a wavefront write to LDS and what others of it read there: the hardware
+// keeps a wavefront's LDS operations in order, and this keeps the compiler to it.
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
 // One operand of a tile: kT rows (m or n) of which `rows` exist.  kStep: bytes of a K
 // step in a "rows" operand.
 template <class E, bool kCols, int kT, int kStep>
@@ -425,12 +431,14 @@ struct Tile {
                                   a[4 * g + 2], a[4 * g + 3]);
             *reinterpret_cast<u32x2*>(chunk<kRowBytes>(at, row, col / 8) + 8 * (lane >> 5)) = v;
           }
+      lanes_meet();
 #pragma unroll 4
       for (int r = 0; r < 32 * kPass; r += kAtOnce) {
         const int row = r + lane / kChunks, c = lane % kChunks;
         put(r0 + 32 * p + row, c0 + 8 * c,
             *reinterpret_cast<const u32x4*>(chunk<kRowBytes>(at, row, c)));
       }
+      lanes_meet();
     }
   }
 
@@ -459,6 +467,7 @@ struct Tile {
             *reinterpret_cast<uint16_t*>(chunk<kRowBytes>(at, col + k, row / 8) + 2 * (row & 7)) =
                 uint16_t(v[k >> 1] >> (16 * (k & 1)));
         }
+    lanes_meet();
 #pragma unroll 4
     for (int c = 0; c < kCols; c += kAtOnce) {
       const int col = c + lane / kChunks, r = lane % kChunks;
@@ -529,12 +538,14 @@ struct Tile {
             *reinterpret_cast<f32x4*>(chunk<kRowBytes>(at, row, col / 4)) =
                 f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]};
           }
+      lanes_meet();
 #pragma unroll
       for (int e = 0; e < kAtOnce; ++e)
         put(p * kAtOnce + e,
             *reinterpret_cast<const f32x4*>(
                 chunk<kRowBytes>(at, e * kAtOnce32 + lane / kChunks32, lane % kChunks32)),
             had[e]);
+      lanes_meet();
     }
   }
 };
