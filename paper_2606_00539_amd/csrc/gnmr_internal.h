@@ -231,6 +231,8 @@ struct Orthogonal {
   int32_t rows, cols, count;
   float ca, cb, cc, eps, scale;
   float held_a, held_p;   // what A and P are multiplied by in fp16 (powers of two)
+  float poly_a, poly_aa, poly_one;  // P as held, of A and A A as held and of I
+  float apply, last;      // X as held, and the result, of P X as held and X's factor
   bool f32;
   // set by launch_orthogonal
   bool flip, first;       // flip: X is the transpose of the update

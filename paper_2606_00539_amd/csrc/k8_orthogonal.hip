@@ -231,9 +231,8 @@ __global__ __launch_bounds__(
   T::product(acc, om, on, K, wave, lane);
   if constexpr (!kIntoX) {
     _Float16* to = kWhat == kGram ? A : P;
-    // (1 / held_a is a power of two, as held_p is)
-    const float s = ldexpf(f * f * a.held_a, -2 * e), per_a = a.held_p / a.held_a;
-    const float p = a.cb * per_a, q = a.cc * (per_a / a.held_a), one = a.ca * a.held_p;
+    const float s = ldexpf(f * f * a.held_a, -2 * e);
+    const float p = a.poly_a, q = a.poly_aa, one = a.poly_one;
     T::change(acc, wave, lane, [&](int group, int m, int n, f32x4 c) {
       if constexpr (kWhat == kGram) return c * s;
       f16x4 h;
@@ -259,7 +258,7 @@ __global__ __launch_bounds__(
     });
   } else if constexpr (kWhat == kApply) {
     _Float16* to = a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np;
-    const float s = ldexpf(f * (kHeld / a.held_p), max(extra - a.spent - a.growth, 0) - e);
+    const float s = ldexpf(f * a.apply, max(extra - a.spent - a.growth, 0) - e);
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
@@ -275,7 +274,7 @@ __global__ __launch_bounds__(
     const int row0 = kFlip ? n0 : m0, col0 = kFlip ? m0 : n0;
     __bf16* out = a.out + int64_t(mat) * a.m * a.n;
     const bool whole = cols % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-    const float s = ldexpf((f * a.scale) / a.held_p, -e);
+    const float s = ldexpf(f * a.last, -e);
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
@@ -376,6 +375,12 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   a.held_a = ldexpf(1.0f, held.a);
   a.held_p = ldexpf(1.0f, held.p);
   a.growth = held.growth;
+  // (all but the coefficients are powers of two)
+  a.poly_a = a.cb * (a.held_p / a.held_a);
+  a.poly_aa = a.cc * (a.held_p / a.held_a / a.held_a);
+  a.poly_one = a.ca * a.held_p;
+  a.apply = kHeld / a.held_p;
+  a.last = a.scale / a.held_p;
   char* w = static_cast<char*>(workspace);
   a.sums = reinterpret_cast<double*>(w);
   a.parts = norm_parts(int64_t(a.rows) * a.cols, a.count);
