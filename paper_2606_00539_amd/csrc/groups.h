@@ -33,7 +33,7 @@ __device__ __forceinline__ bool group_wanted(const GroupArgs& g, int e) {
 
 // Position w of `total` in an order where workgroups w, w + 8, ... (which run on
 // one XCD) take consecutive positions, so that they share panels in its L2.
-__device__ __forceinline__ int xcd_order(int w, int total) {
+__host__ __device__ inline int xcd_order(int w, int total) {
   const int xcd = w % kNumXcd, q = total / kNumXcd, r = total % kNumXcd;
   return xcd * q + (xcd < r ? xcd : r) + w / kNumXcd;
 }
@@ -226,26 +226,76 @@ inline int64_t most_row_tiles(const GroupArgs& g, int kT) {
   return g.rows / kT + std::min<int64_t>(int64_t(g.num) + 1, g.rows);
 }
 
-// Launches a product of grouped rows and N columns: launch(edge, share, workgroups), with
-// *tiles_n set to the tiles side by side.
+// The launches of a product of grouped rows and N columns.
+struct RowLaunch {
+  int tile;       // edge
+  int tiles_n;    // tiles side by side
+  int64_t most;   // tiles, at most
+  bool split;     // of 256 tiles only those of whole rounds, and a launch of the rest in quarters
+};
+inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight) {
+  RowLaunch r{grouped_tile(g, N, K, weight), 0, 0, false};
+  r.tiles_n = (N + r.tile - 1) / r.tile;
+  r.most = most_row_tiles(g, r.tile) * r.tiles_n;
+  if (r.tile < 256) return r;
+  // (without offsets the tiles are known here)
+  r.split = int64_t(K) * weight >= 128 * kSplitSteps &&
+            (g.offsets != nullptr || whole_rounds(int(r.most)) < r.most);
+  return r;
+}
+
+// Makes them: launch(edge, share, workgroups), with *tiles_n set.
 template <class Launch>
 void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* tiles_n,
                       Launch&& launch) {
   using std::integral_constant;
-  const int tile = grouped_tile(g, N, K, weight);
-  *tiles_n = (N + tile - 1) / tile;
-  const int64_t most = most_row_tiles(g, tile) * *tiles_n;
+  const RowLaunch r = row_launch(g, N, K, weight);
+  *tiles_n = r.tiles_n;
   const integral_constant<Share, kAll> all;
-  if (tile == 64) return launch(integral_constant<int, 64>{}, all, most);
-  if (tile == 128) return launch(integral_constant<int, 128>{}, all, most);
-  // (without offsets the tiles are known here)
-  const bool split = int64_t(K) * weight >= 128 * kSplitSteps &&
-                     (g.offsets != nullptr || whole_rounds(int(most)) < most);
-  if (!split) return launch(integral_constant<int, 256>{}, all, most);
-  if (g.offsets != nullptr || whole_rounds(int(most)) > 0)
-    launch(integral_constant<int, 256>{}, integral_constant<Share, kRounds>{}, most);
+  if (r.tile == 64) return launch(integral_constant<int, 64>{}, all, r.most);
+  if (r.tile == 128) return launch(integral_constant<int, 128>{}, all, r.most);
+  if (!r.split) return launch(integral_constant<int, 256>{}, all, r.most);
+  launch(integral_constant<int, 256>{}, integral_constant<Share, kRounds>{}, r.most);
   launch(integral_constant<int, 128>{}, integral_constant<Share, kRest>{},
-         std::min<int64_t>(4 * most, 512));
+         std::min<int64_t>(4 * r.most, 512));
+}
+
+// Tile *v of group *e for workgroup w, of `num` groups with `per` tiles each.  Where a group has
+// tiles enough, every XCD (workgroups w, w + 8, ... run on one) takes an eighth of each group's, so
+// that groups of many rows keep all of them busy; false where its eighth is a tile shorter.  64
+// experts 2048 x 1408 (176 tiles each), fp32, over two micro-batches of uneven load: with whole
+// groups to an XCD 733 us, with eighths 672; one call of even load 201 and 218.  Four experts of 80 x
+// 136 (2 tiles each) 15.3 and 19.0.
+constexpr int kSharedTiles = 64;
+__host__ __device__ constexpr int slots_of(int num, int per) {
+  constexpr int kXcds = kNumXcd;
+  return num == 1 || per < kSharedTiles ? per : (per + kXcds - 1) / kXcds * kXcds;
+}
+__host__ __device__ inline bool share_of(int w, int num, int per, int* v, int* e) {
+  if (num == 1 || per < kSharedTiles) {
+    const int at = xcd_order(w, num * per);
+    *e = at / per;
+    *v = at % per;
+    return true;
+  }
+  constexpr int kXcds = kNumXcd;
+  const int slots = slots_of(num, per) / kXcds, i = w / kXcds, at = i % slots;
+  *e = i / slots;
+  const int xcd = (w + *e) % kXcds, q = per / kXcds, r = per % kXcds;
+  *v = xcd * q + (xcd < r ? xcd : r) + at;
+  return at < q + (xcd < r ? 1 : 0);
+}
+
+// The tile edge of the gradients of M x N matrices.
+inline int wgrad_tile(const GroupArgs& g, int M, int N) {
+  // 256 tiles where experts have rows enough to outweigh what a tile takes beside its
+  // steps, and tiles enough for the chip.  us in 128 and 256 tiles, bf16 and accumulating (all
+  // through the caches; past them the first are 178, 714 and 931 as chosen): 64
+  // experts 2048 x 1408 of 384 rows 269 and 282, 319 and 621; 8 of 4096 x 11008 of 1,024
+  // rows 861 and 855, 980 and 1,543; one of 5120 x 13824 of 8,192 rows 1,524 and 951, 1,483 and
+  // 1,096; one of 4096 x 4096 of 4,096 rows 130 and 109, 142 and 133.
+  const int64_t tiles = int64_t(g.num) * ((M + 255) / 256) * ((N + 255) / 256);
+  return g.rows / g.num >= 2048 && tiles >= 192 ? 256 : 128;
 }
 
 }  // namespace gnmr

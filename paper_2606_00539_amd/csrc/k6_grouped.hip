@@ -70,32 +70,6 @@ struct WgradTile {
   using T = mm::Tile<Bf16, true, true, kT, kT, 2, 64, kPerCu == 3 ? 3 : 4>;
 };
 
-// Tile *v of group *e for workgroup w, of `num` groups with `per` tiles each.  Where a group has
-// tiles enough, every XCD (workgroups w, w + 8, ... run on one) takes an eighth of each group's, so
-// that groups of many rows keep all of them busy; false where its eighth is a tile shorter.  64
-// experts 2048 x 1408 (176 tiles each), fp32, over two micro-batches of uneven load: with whole
-// groups to an XCD 733 us, with eighths 672; one call of even load 201 and 218.  Four experts of 80 x
-// 136 (2 tiles each) 15.3 and 19.0.
-constexpr int kSharedTiles = 64;
-__host__ __device__ constexpr int slots_of(int num, int per) {
-  constexpr int kXcds = kNumXcd;
-  return num == 1 || per < kSharedTiles ? per : (per + kXcds - 1) / kXcds * kXcds;
-}
-__device__ __forceinline__ bool share_of(int w, int num, int per, int* v, int* e) {
-  if (num == 1 || per < kSharedTiles) {
-    const int at = xcd_order(w, num * per);
-    *e = at / per;
-    *v = at % per;
-    return true;
-  }
-  constexpr int kXcds = kNumXcd;
-  const int slots = slots_of(num, per) / kXcds, i = w / kXcds, at = i % slots;
-  *e = i / slots;
-  const int xcd = (w + *e) % kXcds, q = per / kXcds, r = per % kXcds;
-  *v = xcd * q + min(xcd, r) + at;
-  return at < q + (xcd < r ? 1 : 0);
-}
-
 template <bool kF32, bool kAcc, int kT>
 __global__ __launch_bounds__(mm::kThreads, (WgradTile<kF32, kAcc, kT>::kPerCu)) void k6_wgrad(
     const GroupedWgrad a) {
@@ -219,14 +193,7 @@ void launch_wgrad_of(GroupedWgrad a, hipStream_t s) {
                        dim3(unsigned(int64_t(a.g.num) * slots_of(a.g.num, a.tiles_m * a.tiles_n))),
                        dim3(mm::kThreads), 0, s, a);
   };
-  // 256 tiles where experts have rows enough to outweigh what a tile takes beside its
-  // steps, and tiles enough for the chip.  us in 128 and 256 tiles, bf16 and accumulating (all
-  // through the caches; past them the first are 178, 714 and 931 as chosen): 64
-  // experts 2048 x 1408 of 384 rows 269 and 282, 319 and 621; 8 of 4096 x 11008 of 1,024
-  // rows 861 and 855, 980 and 1,543; one of 5120 x 13824 of 8,192 rows 1,524 and 951, 1,483 and
-  // 1,096; one of 4096 x 4096 of 4,096 rows 130 and 109, 142 and 133.
-  const int64_t tiles = int64_t(a.g.num) * ((a.M + 255) / 256) * ((a.N + 255) / 256);
-  if (a.g.rows / a.g.num >= 2048 && tiles >= 192) launch(std::integral_constant<int, 256>{});
+  if (wgrad_tile(a.g, a.M, a.N) == 256) launch(std::integral_constant<int, 256>{});
   else launch(std::integral_constant<int, 128>{});
 }
 
