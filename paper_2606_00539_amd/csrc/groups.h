@@ -220,6 +220,39 @@ inline int grouped_tile(const GroupArgs& g, int N, int K, int weight) {
   return us64 <= us128 && us64 <= us256 ? 64 : us128 <= us256 ? 128 : 256;
 }
 
+// The launches of a batch of products of K8: X X^T and A A, symmetric (tiles on and above the
+// diagonal), and P X, with X m x n.
+enum class BatchProduct { kOfRows, kOfSquares, kOntoRows };
+struct BatchLaunch {
+  int64_t all, large;   // tiles of 256, and how many of them, from the first, run as such
+  int edge;             // of the tiles that the others are cut into (0: there are none)
+};
+// All tiles of one edge, or 256 tiles in whole rounds over the chip and the rest, which would not
+// fill another, in smaller ones; whichever takes the least by us_of_tiles.
+inline BatchLaunch batch_launch(BatchProduct what, int count, int m, int n) {
+  const bool square = what != BatchProduct::kOntoRows;
+  // tiles of an edge that lie in the products; of the smaller ones a share makes up the rest
+  auto tiles = [&](double t) {
+    const double h = ceil(m / t), w = ceil(n / t);
+    return count * (square ? h * (h + 1) / 2 : h * w);
+  };
+  const int64_t all = int64_t(tiles(256.0)), rest = all % 256;
+  const double steps = (what == BatchProduct::kOfRows ? n : m) / 64;
+  const double share = double(rest) / double(all), kLaunch = 4.0;
+  const double bytes = 2.0 * count * m * (what == BatchProduct::kOfRows      ? n + m
+                                          : what == BatchProduct::kOfSquares ? 2.0 * m
+                                                                             : m + 2.0 * n);
+  const double whole = us_of_tiles<256>(double(all - rest), steps, bytes) + kLaunch;
+  const double us[5] = {us_of_tiles<64>(tiles(64.0), steps, bytes),
+                        us_of_tiles<128>(tiles(128.0), steps, bytes),
+                        us_of_tiles<256>(double(all), steps, bytes),
+                        whole + us_of_tiles<64>(share * tiles(64.0), steps, bytes),
+                        whole + us_of_tiles<128>(share * tiles(128.0), steps, bytes)};
+  const int best = int(std::min_element(us, us + (rest < all && rest > 0 ? 5 : 3)) - us);
+  return BatchLaunch{all, best < 2 ? 0 : best == 2 ? all : all - rest,
+                     best == 2 ? 0 : best == 0 || best == 3 ? 64 : 128};
+}
+
 // Tiles of kT rows that `rows` rows in g.num groups (and the rest) can make at most.
 inline int64_t most_row_tiles(const GroupArgs& g, int kT) {
   if (g.offsets == nullptr) return (int64_t(g.rows) + kT - 1) / kT;

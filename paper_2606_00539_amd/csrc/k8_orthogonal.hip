@@ -306,36 +306,19 @@ void launch_tiles(Orthogonal a, int64_t first, int64_t n, hipStream_t s) {
                      dim3(mm::kThreads), 0, s, a);
 }
 
-// A product's tiles: all of one edge, or 256 tiles in whole rounds over the chip and the rest,
-// which would not fill another, in smaller ones; whichever takes the least by us_of_tiles.
 template <int kWhat, bool kFlip>
 void launch_product(Orthogonal a, hipStream_t s) {
   constexpr bool kSquare = kWhat == kGram || kWhat == kPoly;
   a.tiles_m = (a.mp + 255) / 256;
   a.tiles_n = kSquare ? a.tiles_m : (a.np + 255) / 256;
   a.tiles = kSquare ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
-  const int64_t all = int64_t(a.count) * a.tiles, rest = all % 256;
-  const double steps = (kWhat == kGram ? a.np : a.mp) / 64;
-  // smaller tiles that lie in the product, the share of them in the rest
-  auto tiles = [&](double t) {
-    const double m = ceil(a.mp / t), n = ceil(a.np / t);
-    return a.count * (kSquare ? m * (m + 1) / 2 : m * n);
-  };
-  const double share = double(rest) / double(all), kLaunch = 4.0;
-  const double bytes = 2.0 * a.count * a.mp * (kWhat == kGram   ? a.np + a.mp
-                                                  : kWhat == kPoly ? 2.0 * a.mp
-                                                                   : a.mp + 2.0 * a.np);
-  const double whole = us_of_tiles<256>(double(all - rest), steps, bytes) + kLaunch;
-  const double us[5] = {us_of_tiles<64>(tiles(64.0), steps, bytes),
-                        us_of_tiles<128>(tiles(128.0), steps, bytes),
-                        us_of_tiles<256>(double(all), steps, bytes),
-                        whole + us_of_tiles<64>(share * tiles(64.0), steps, bytes),
-                        whole + us_of_tiles<128>(share * tiles(128.0), steps, bytes)};
-  const int best = int(std::min_element(us, us + (rest < all && rest > 0 ? 5 : 3)) - us);
-  const int64_t large = best < 2 ? 0 : best == 2 ? all : all - rest;
-  launch_tiles<kWhat, kFlip, 256>(a, 0, large, s);
-  if (best == 0 || best == 3) launch_tiles<kWhat, kFlip, 64>(a, large, all - large, s);
-  else launch_tiles<kWhat, kFlip, 128>(a, large, all - large, s);
+  const BatchLaunch b = batch_launch(kWhat == kGram   ? BatchProduct::kOfRows
+                                     : kWhat == kPoly ? BatchProduct::kOfSquares
+                                                      : BatchProduct::kOntoRows,
+                                     a.count, a.mp, a.np);
+  launch_tiles<kWhat, kFlip, 256>(a, 0, b.large, s);
+  if (b.edge == 64) launch_tiles<kWhat, kFlip, 64>(a, b.large, b.all - b.large, s);
+  else launch_tiles<kWhat, kFlip, 128>(a, b.large, b.all - b.large, s);
 }
 
 int pad(int x) { return (x + 63) / 64 * 64; }

@@ -1,5 +1,5 @@
-"""Shapes of the grouped products by the kernel that they run in.  test_expert_tiles.py checks on
-the CPU that each still does, test_gpu_expert_tiles.py runs them."""
+"""Shapes of the grouped products and of the orthogonalisation's by the kernels that they run in.
+test_expert_tiles.py checks on the CPU that each still does, test_gpu_expert_tiles.py runs them."""
 import os
 import subprocess
 
@@ -12,7 +12,7 @@ PROGRAM = """
 #include <stdio.h>
 #include <string.h>
 #include "groups.h"
-// op rows groups(0: one without offsets) out in -> what runs
+// op rows groups(0: one without offsets) out in, or "batch" count m n and a 0 -> what runs
 int main() {
   char op[16];
   int rows, groups, out, in;
@@ -20,6 +20,17 @@ int main() {
   while (scanf("%15s %d %d %d %d", op, &rows, &groups, &out, &in) == 5) {
     const gnmr::GroupArgs g{groups == 0 ? nullptr : &kOffsets, nullptr, groups == 0 ? 1 : groups, 1,
                             rows};
+    if (!strcmp(op, "batch")) {
+      for (auto what : {gnmr::BatchProduct::kOfRows, gnmr::BatchProduct::kOfSquares,
+                        gnmr::BatchProduct::kOntoRows}) {
+        const gnmr::BatchLaunch b =
+            gnmr::batch_launch(what, rows, (groups + 63) / 64 * 64, (out + 63) / 64 * 64);
+        printf(b.large == 0 ? "%s%d" : b.edge == 0 ? "%s256" : "%s256+%d",
+               what == gnmr::BatchProduct::kOfRows ? "" : " ", b.edge);
+      }
+      puts("");
+      continue;
+    }
     if (!strcmp(op, "wgrad")) {
       const int edge = gnmr::wgrad_tile(g, out, in);
       const int per = (out + edge - 1) / edge * ((in + edge - 1) / edge);
@@ -104,3 +115,17 @@ def shape(which, name):
     rows = pad if counts is None else sum(counts) + pad
     return which, rows, 0 if counts is None else len(counts), *(
         (K, N) if which == "dgrad" else (N, K))
+
+
+# count, m, n, and what A = X X^T, P and P X run in
+BATCH = [
+    (1, 40, 40, "64 64 64"),
+    (53, 195, 197, "128 128 128"),
+    (57, 391, 431, "256 256 256"),
+    (51, 663, 1995, "256+128 128 256"),
+    (49, 643, 1353, "256+64 128 128"),
+    (7, 2112, 2250, "256+128 256+128 256+128"),
+    (19, 1154, 1155, "256+64 256+64 256"),
+    (4, 923, 4275, "64 64 256+64"),
+    (3, 1966, 3098, "128 128 256+128"),
+]

@@ -26,6 +26,13 @@ def test_the_shapes_run_where_they_are_meant_to(tiles):
         assert {g for (v, _), g in zip(names, got) if v == w} == every
 
 
+def test_the_batches_run_where_they_are_meant_to(tiles):
+    got = tiles([("batch", count, m, n, 0) for count, m, n, _ in T.BATCH])
+    assert got == [want for *_, want in T.BATCH]
+    every = {"64", "128", "256", "256+64", "256+128"}
+    assert all({g.split()[k] for g in got} == every for k in range(3))
+
+
 PROGRAM = """
 #include <stdio.h>
 #include <vector>

@@ -1,6 +1,7 @@
-"""The grouped products in each kernel that the rules choose (expert_tiles.py), with a mask over
-uneven experts, rows of nobody holding NaN and depths that end inside a step, against the formulas
-in float64 on the device.  Tolerances as in test_gpu_experts.py."""
+"""The grouped products and the orthogonalisation in each kernel that the rules choose
+(expert_tiles.py), with a mask over uneven experts, rows of nobody holding NaN and sizes that end
+inside a step or a tile, against the formulas in float64 on the device.  Tolerances as in
+test_gpu_experts.py."""
 import numpy as np
 import pytest
 
@@ -90,3 +91,23 @@ def test_weight_gradients(dtype, name):
             sq = torch.nn.functional.pad(sq, (0, -i % 128, 0, -o % 128))
             blocks = sq.view(-(-o // 128), 128, -(-i // 128), 128).sum((1, 3)).flatten()
             assert bool(((parts[e].double() - blocks).abs() <= 300 * 2.0 ** -24 * blocks).all()), e
+
+
+@pytest.mark.parametrize("flip", [False, True])
+@pytest.mark.parametrize("count,m,n,runs", T.BATCH)
+def test_orthogonalize(count, m, n, runs, flip):
+    torch, t = ops()
+    print("orthogonalize", count, m, n, flip, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(33)
+    x = (torch.randn(count, m, n, generator=g, device="cuda") * 1e-3).to(torch.bfloat16)
+    given = x.transpose(1, 2).contiguous() if flip else x
+    got = t.orthogonalize(given)
+    a, b, c = 3.4445, -4.7750, 2.0315
+    for k in sorted({0, count // 2, count - 1}):
+        v = x[k].double()
+        v = v / (v.square().sum().sqrt() + 1e-7)
+        for _ in range(5):
+            s = v @ v.t().contiguous()
+            v = a * v + (b * s + c * (s @ s)) @ v
+        y = got[k].double()
+        assert float(((y.t() if flip else y) - v).norm()) <= 0.00825 * float(v.norm()), k
