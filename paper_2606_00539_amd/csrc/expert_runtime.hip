@@ -316,15 +316,11 @@ gnmr_status gnmr_orthogonalize(const void* in, int32_t in_dtype, void* out, int3
     a.rows = rows;
     a.cols = cols;
     a.count = count;
-    a.ca = z.a;
-    a.cb = z.b;
-    a.cc = z.c;
     a.eps = z.eps;
-    a.scale = z.scale;
     a.f32 = in_dtype == GNMR_F32;
     if (gnmr::orthogonal_workgroups(a) > kMaxWorkgroups)
       return fail(GNMR_E_INVALID, "too many output tiles for one launch");
-    GNMR_HIP(gnmr::launch_orthogonal(a, workspace, z.steps, static_cast<hipStream_t>(stream)));
+    GNMR_HIP(gnmr::launch_orthogonal(a, z, workspace, static_cast<hipStream_t>(stream)));
     return GNMR_OK;
   });
 }

@@ -225,28 +225,32 @@ hipError_t launch_quantize_rows(const QuantizeRows& a, bool f32, hipStream_t s);
 hipError_t launch_quantized_linear(QuantizedLinear a, hipStream_t s);
 
 // K8 (orthogonalisation; see k8_orthogonal.hip)
+struct OrthogonalStart {  // of a matrix: X = factor * 2^-extra * what is held
+  float factor;
+  int32_t extra;
+};
 struct Orthogonal {
   const void* in;         // [count][rows][cols] bf16 or fp32
   __bf16* out;            // [count][rows][cols]
   int32_t rows, cols, count;
-  float ca, cb, cc, eps, scale;
-  float held_a, held_p;   // what A and P are multiplied by in fp16 (powers of two)
-  float poly_a, poly_aa, poly_one;  // P as held, of A and A A as held and of I
-  float apply, last;      // X as held, and the result, of P X as held and X's factor
+  float eps;
   bool f32;
   // set by launch_orthogonal
-  bool flip, first;       // flip: X is the transpose of the update
-  int32_t m, n, mp, np, now, tiles_m, tiles_n, tiles, first_tile, num_tiles;
+  bool flip;              // X is the transpose of the update
+  int32_t m, n, mp, np, step, tiles_m, tiles_n, tiles, first_tile, num_tiles;
   int32_t parts;
-  int32_t growth, spent;  // what a step takes off `extra`, and the steps before have taken
+  int32_t growth;         // what a step takes off `extra`
+  float held_a;           // what A is multiplied by in fp16
+  float poly_a, poly_aa, poly_one;  // P as held, of A and A A as held and of I
+  float apply, last;      // X as held, and the result, of P X as held and X's factor
   double* sums;           // [count][parts], partial sums of squares
-  float* factor;          // [count], first iteration: X = factor * 2^-extra * what is held
-  int32_t* extra;         // [count], powers of two that X is held higher by at first
+  OrthogonalStart* start; // [count]
   _Float16* x[2];         // [count][mp][np]
   _Float16 *A, *P;        // [count][mp][mp]
 };
 int64_t orthogonal_workgroups(const Orthogonal& a);
 int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count);
-hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream_t s);
+hipError_t launch_orthogonal(Orthogonal a, const gnmr_newton_schulz& z, void* workspace,
+                             hipStream_t s);
 
 }  // namespace gnmr

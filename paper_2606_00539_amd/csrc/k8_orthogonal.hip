@@ -128,10 +128,8 @@ __global__ __launch_bounds__(256) void k8_load(const Orthogonal a) {
     --extra;                        // length * 2^extra <= norm (0 where length is infinite)
   }
   const int up = 12 - k + extra;    // |G| * 2^up <= 2^12
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-    a.factor[mat] = norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, 12 - k));
-    a.extra[mat] = extra;
-  }
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+    a.start[mat] = OrthogonalStart{norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, 12 - k)), extra};
   // eight consecutive elements of a row of G to a lane: rows r0 .. r0+63 from column c0
   const char* in = static_cast<const char*>(a.in) + int64_t(mat) * size * kSize;
   const int r0 = kFlip ? n0 : m0, c0 = kFlip ? m0 : n0;
@@ -204,7 +202,7 @@ __global__ __launch_bounds__(
   const int m0 = tm * kT, n0 = tn * kT;
   if (m0 >= a.mp || n0 >= (kIntoX ? a.np : a.mp) || (!kIntoX && tm > tn)) return;
   const int K = kWhat == kGram ? a.np : a.mp;
-  const _Float16* x = a.x[a.now] + int64_t(mat) * a.mp * a.np;
+  const _Float16* x = a.x[a.step & 1] + int64_t(mat) * a.mp * a.np;
   _Float16* A = a.A + int64_t(mat) * a.mp * a.mp;
   _Float16* P = a.P + int64_t(mat) * a.mp * a.mp;
   const _Float16* left = kWhat == kGram ? x : kWhat == kPoly ? A : P;
@@ -226,8 +224,9 @@ __global__ __launch_bounds__(
   f16x4 old[kEarly ? T::kGroups : 1];
   if constexpr (kEarly)
     T::groups(wave, lane, [&](int e, int m, int n) { old[e] = stored(m, n); });
-  const float f = a.first ? a.factor[mat] : kUnheld;   // X = f * 2^-e * what is held
-  const int extra = a.extra[mat], e = max(extra - a.spent, 0);
+  const OrthogonalStart start = a.start[mat];
+  const float f = a.step == 0 ? start.factor : kUnheld;   // X = f * 2^-e * what is held
+  const int extra = start.extra - a.step * a.growth, e = max(extra, 0);
   T::product(acc, om, on, K, wave, lane);
   if constexpr (!kIntoX) {
     _Float16* to = kWhat == kGram ? A : P;
@@ -257,8 +256,8 @@ __global__ __launch_bounds__(
         *reinterpret_cast<u32x4*>(to + int64_t(n0 + n) * a.mp + m0 + m) = h;
     });
   } else if constexpr (kWhat == kApply) {
-    _Float16* to = a.x[a.now ^ 1] + int64_t(mat) * a.mp * a.np;
-    const float s = ldexpf(f * a.apply, max(extra - a.spent - a.growth, 0) - e);
+    _Float16* to = a.x[(a.step & 1) ^ 1] + int64_t(mat) * a.mp * a.np;
+    const float s = ldexpf(f * a.apply, max(extra - a.growth, 0) - e);
     T::out16(
         acc, wave, lane,
         [&](int, int, float a0, float a1, float a2, float a3) {
@@ -345,33 +344,32 @@ int norm_parts(int64_t size, int count) {
 int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count) {
   const int64_t mp = pad(std::min(rows, cols)), np = pad(std::max(rows, cols));
   return up256(int64_t(count) * norm_parts(int64_t(rows) * cols, count) * 8) +
-         2 * up256(int64_t(count) * 4) + int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
+         up256(int64_t(count) * int64_t(sizeof(OrthogonalStart))) + int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
 }
 
-hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream_t s) {
+hipError_t launch_orthogonal(Orthogonal a, const gnmr_newton_schulz& z, void* workspace,
+                             hipStream_t s) {
   a.flip = a.rows > a.cols;
   a.m = a.flip ? a.cols : a.rows;
   a.n = a.flip ? a.rows : a.cols;
   a.mp = pad(a.m);
   a.np = pad(a.n);
-  const HeldExponents held = held_exponents(a.ca, a.cb, a.cc, steps);
+  const HeldExponents held = held_exponents(z.a, z.b, z.c, z.steps);
   a.held_a = ldexpf(1.0f, held.a);
-  a.held_p = ldexpf(1.0f, held.p);
+  const float held_p = ldexpf(1.0f, held.p);
   a.growth = held.growth;
   // (all but the coefficients are powers of two)
-  a.poly_a = a.cb * (a.held_p / a.held_a);
-  a.poly_aa = a.cc * (a.held_p / a.held_a / a.held_a);
-  a.poly_one = a.ca * a.held_p;
-  a.apply = kHeld / a.held_p;
-  a.last = a.scale / a.held_p;
+  a.poly_a = z.b * (held_p / a.held_a);
+  a.poly_aa = z.c * (held_p / a.held_a / a.held_a);
+  a.poly_one = z.a * held_p;
+  a.apply = kHeld / held_p;
+  a.last = z.scale / held_p;
   char* w = static_cast<char*>(workspace);
   a.sums = reinterpret_cast<double*>(w);
   a.parts = norm_parts(int64_t(a.rows) * a.cols, a.count);
   w += up256(int64_t(a.count) * a.parts * 8);
-  a.factor = reinterpret_cast<float*>(w);
-  w += up256(int64_t(a.count) * 4);
-  a.extra = reinterpret_cast<int32_t*>(w);
-  w += up256(int64_t(a.count) * 4);
+  a.start = reinterpret_cast<OrthogonalStart*>(w);
+  w += up256(int64_t(a.count) * int64_t(sizeof(OrthogonalStart)));
   const int64_t xs = int64_t(a.count) * a.mp * a.np, as = int64_t(a.count) * a.mp * a.mp;
   a.x[0] = reinterpret_cast<_Float16*>(w);
   a.x[1] = a.x[0] + xs;
@@ -385,13 +383,10 @@ hipError_t launch_orthogonal(Orthogonal a, void* workspace, int steps, hipStream
   else if (a.f32) hipLaunchKernelGGL((k8_load<true, false>), tiles, dim3(256), 0, s, a);
   else if (a.flip) hipLaunchKernelGGL((k8_load<false, true>), tiles, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k8_load<false, false>), tiles, dim3(256), 0, s, a);
-  for (int i = 0; i < steps; ++i) {
-    a.first = i == 0;
-    a.now = i & 1;
-    a.spent = i * a.growth;
+  for (a.step = 0; a.step < z.steps; ++a.step) {
     launch_product<kGram, false>(a, s);
     launch_product<kPoly, false>(a, s);
-    if (i + 1 < steps) launch_product<kApply, false>(a, s);
+    if (a.step + 1 < z.steps) launch_product<kApply, false>(a, s);
     else if (a.flip) launch_product<kLast, true>(a, s);
     else launch_product<kLast, false>(a, s);
   }
