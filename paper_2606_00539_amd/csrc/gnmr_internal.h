@@ -245,6 +245,8 @@ struct Orthogonal {
   float apply, last;      // X as held, and the result, of P X as held and X's factor
   double* sums;           // [count][parts], partial sums of squares
   OrthogonalStart* start; // [count]
+  float* gap;             // [count][mp], what rounding took from A's diagonal as held
+  float* row;             // [count][mp], what the rows of P as held are multiplied by
   _Float16* x[2];         // [count][mp][np]
   _Float16 *A, *P;        // [count][mp][mp]
 };

@@ -9,17 +9,24 @@
 //
 // The iterates are held in fp16 between the products, X scaled by 2^12: |X| <= its
 // largest singular value, so the range holds values from 2^-26 (with all 11 bits) to 15.99, and each
-// product's rounding is 2^-12 relative, an eighth of bf16's at the same matrix-core rate.  |A| can
+// rounding is at most 2^-11 relative, an eighth of bf16's at the same matrix-core rate.  |A| can
 // reach the square of that value and |P| what the polynomial makes of it: their powers of two follow
 // from the coefficients (k8_range.h), 2^12 too with the usual ones, whose |A| stays below 1.5
 // and |P| below 4.  With lower ones their small values lose bits, but A and P act as wholes: what
-// counts is the rounding beside their largest.  Products
-// accumulate in fp32.  a is part of P's diagonal and is rounded with it, to 2^-12
-// of at most a: as much again as X's own rounding, and less than the error of the
-// result in bf16; added to the product in fp32 it would cost a read of X for every
-// product (64 updates of 1408 x 2048: 640 us a product, 540 without).  The first X is
-// G times a power of two, exact for bf16 input; what is left of the norm goes into the
-// first iteration's factors.  The norm is summed in float64.
+// counts is the rounding beside their largest.  Products accumulate in fp32.
+//
+// The diagonals are kept whole, for they are the largest entries and, in an update much wider than
+// high, nearly equal: their roundings went one way in every row and step, and made most of the
+// error.  What rounding takes off A's diagonal (d) is put back into P's in fp32, as b d + 2 c A_ii d
+// (off the diagonal it is as small as the entries' own rounding); and P is held as D P' with P'
+// rounded and D, next to I, such that D P' has P's diagonal: D multiplies the rows of the product.
+// Error in the 2-norm before and after, of which the last rounding to bf16 is 1.66e-3: 32 x 1673
+// 3.2e-3 and 1.8e-3, 256 x 256 2.1e-3 and 1.9e-3, 1408 x 2048 1.89e-3 and 1.83e-3; 64 updates of 1408 x
+// 2048 take 1% longer so, 16 of 256 x 256 2%.  (a X added to the product in fp32, instead of a in
+// P's diagonal, costs a read of X for every product, 640 us instead of 540, and is no nearer.)
+//
+// The first X is G times a power of two, exact for bf16 input; what is left of the norm goes into
+// the first iteration's factors.  The norm is summed in float64.
 // Where eps is larger than the norm, X starts that much below 1 and is held as many powers of two
 // higher, fewer by every step by what it may grow: it keeps its bits however small.
 #include "gnmr_internal.h"
@@ -128,8 +135,12 @@ __global__ __launch_bounds__(256) void k8_load(const Orthogonal a) {
     --extra;                        // length * 2^extra <= norm (0 where length is infinite)
   }
   const int up = 12 - k + extra;    // |G| * 2^up <= 2^12
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-    a.start[mat] = OrthogonalStart{norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, 12 - k)), extra};
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    // The factor is kept to 20 bits (X to 5e-7 of its scale): the last bit of a norm, which a
+    // product with 2^20 that is off by as much changes, then leaves every bit of the result.
+    const float f = norm == 0.0 ? 0.0f : float(1.0 / ldexp(norm, 12 - k));
+    a.start[mat] = OrthogonalStart{__uint_as_float((__float_as_uint(f) + 8u) & ~15u), extra};
+  }
   // eight consecutive elements of a row of G to a lane: rows r0 .. r0+63 from column c0
   const char* in = static_cast<const char*>(a.in) + int64_t(mat) * size * kSize;
   const int r0 = kFlip ? n0 : m0, c0 = kFlip ? m0 : n0;
@@ -227,20 +238,63 @@ __global__ __launch_bounds__(
   const OrthogonalStart start = a.start[mat];
   const float f = a.step == 0 ? start.factor : kUnheld;   // X = f * 2^-e * what is held
   const int extra = start.extra - a.step * a.growth, e = max(extra, 0);
+  // What the epilogue needs of a lane's rows is on its way while the product runs (rows past the
+  // last ones read that: nothing of theirs is stored).
+  float* const gap = a.gap + int64_t(mat) * a.mp;
+  float* const row = a.row + int64_t(mat) * a.mp;
+  constexpr bool kOfRows = kWhat == kPoly || (kIntoX && !kFlip);
+  float of[kOfRows ? T::kRows / 32 : 1];
+  if constexpr (kOfRows) {
+#pragma unroll
+    for (int i = 0; i < T::kRows / 32; ++i)
+      of[i] = (kWhat == kPoly ? gap : row)[min(m0 + T::first_row(wave) + 32 * i + (lane & 31),
+                                               a.mp - 1)];
+  }
   T::product(acc, om, on, K, wave, lane);
+  // s times P's factors for four accumulators at (row, col) of the tile
+  auto factors = [&](float s, int r, int c) {
+    if constexpr (kFlip) {
+      return s * *reinterpret_cast<const f32x4*>(row + min(m0 + c, a.mp - 4));
+    } else {
+      const float v = s * of[kOfRows ? uint32_t(r - T::first_row(wave)) / 32 : 0];
+      return f32x4{v, v, v, v};
+    }
+  };
   if constexpr (!kIntoX) {
     _Float16* to = kWhat == kGram ? A : P;
     const float s = ldexpf(f * f * a.held_a, -2 * e);
     const float p = a.poly_a, q = a.poly_aa, one = a.poly_one;
     T::change(acc, wave, lane, [&](int group, int m, int n, f32x4 c) {
-      if constexpr (kWhat == kGram) return c * s;
-      f16x4 h;
-      if constexpr (kEarly) h = old[group];
-      else h = stored(m, n);
+      // which of the four is on the diagonal, which the lane's blocks of 32 on their own meet
+      constexpr int kAcross = T::kCols / 32;
+      const uint32_t on = uint32_t(m0 + m - n0 - n);
+      const bool meets = group / 4 / kAcross == group / 4 % kAcross && on < 4;
       f32x4 r;
+      float h = 0.0f;
+      if constexpr (kWhat == kGram) {
+        r = c * s;
+      } else {
+        f16x4 v;
+        if constexpr (kEarly) v = old[group];
+        else v = stored(m, n);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        r[k] = p * float(h[k]) + q * c[k] + (m0 + m == n0 + n + k ? one : 0.0f);
+        for (int k = 0; k < 4; ++k) {
+          r[k] = p * float(v[k]) + q * c[k];
+          h = on == uint32_t(k) ? float(v[k]) : h;
+        }
+      }
+      if (meets && m0 + m < a.mp) {
+        float d = on == 0 ? r[0] : on == 1 ? r[1] : on == 2 ? r[2] : r[3];
+        if constexpr (kWhat == kGram) {
+          gap[m0 + m] = d - float(_Float16(d));
+        } else {
+          d += one + of[kWhat == kPoly ? group / 4 / kAcross : 0] * (p + 2.0f * q * h);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) r[k] = on == uint32_t(k) ? d : r[k];
+          const float held = float(_Float16(d));
+          row[m0 + m] = fabsf(held) < 0x1p-14f ? 1.0f : d / held;
+        }
+      }
       return r;
     });
     auto round = [](int, int, float a0, float a1, float a2, float a3) {
@@ -260,8 +314,9 @@ __global__ __launch_bounds__(
     const float s = ldexpf(f * a.apply, max(extra - a.growth, 0) - e);
     T::out16(
         acc, wave, lane,
-        [&](int, int, float a0, float a1, float a2, float a3) {
-          return half4(s * a0, s * a1, s * a2, s * a3);
+        [&](int r, int c, float a0, float a1, float a2, float a3) {
+          const f32x4 v = factors(s, r, c);
+          return half4(v[0] * a0, v[1] * a1, v[2] * a2, v[3] * a3);
         },
         [&](int m, int n, const u32x4& h) {
           if (m0 + m < a.mp && n0 + n < a.np)
@@ -276,8 +331,9 @@ __global__ __launch_bounds__(
     const float s = ldexpf(f * a.last, -e);
     T::out16(
         acc, wave, lane,
-        [&](int, int, float a0, float a1, float a2, float a3) {
-          return u32x2{pack(s * a0, s * a1), pack(s * a2, s * a3)};
+        [&](int r, int c, float a0, float a1, float a2, float a3) {
+          const f32x4 v = factors(s, r, c);
+          return u32x2{pack(v[0] * a0, v[1] * a1), pack(v[2] * a2, v[3] * a3)};
         },
         [&](int row, int col, const u32x4& h) {
           const int r = row0 + row, c = col0 + col;
@@ -344,7 +400,8 @@ int norm_parts(int64_t size, int count) {
 int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count) {
   const int64_t mp = pad(std::min(rows, cols)), np = pad(std::max(rows, cols));
   return up256(int64_t(count) * norm_parts(int64_t(rows) * cols, count) * 8) +
-         up256(int64_t(count) * int64_t(sizeof(OrthogonalStart))) + int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
+         up256(int64_t(count) * int64_t(sizeof(OrthogonalStart))) + 2 * up256(count * mp * 4) +
+         int64_t(count) * (2 * mp * np + 2 * mp * mp) * 2;
 }
 
 hipError_t launch_orthogonal(Orthogonal a, const gnmr_newton_schulz& z, void* workspace,
@@ -370,6 +427,10 @@ hipError_t launch_orthogonal(Orthogonal a, const gnmr_newton_schulz& z, void* wo
   w += up256(int64_t(a.count) * a.parts * 8);
   a.start = reinterpret_cast<OrthogonalStart*>(w);
   w += up256(int64_t(a.count) * int64_t(sizeof(OrthogonalStart)));
+  a.gap = reinterpret_cast<float*>(w);
+  w += up256(int64_t(a.count) * a.mp * 4);
+  a.row = reinterpret_cast<float*>(w);
+  w += up256(int64_t(a.count) * a.mp * 4);
   const int64_t xs = int64_t(a.count) * a.mp * a.np, as = int64_t(a.count) * a.mp * a.mp;
   a.x[0] = reinterpret_cast<_Float16*>(w);
   a.x[1] = a.x[0] + xs;
