@@ -181,8 +181,10 @@ class ExpertUnits:
 
     def linear(self, name, x, offsets):
         k = self._index[name]
-        use, weight = _Use(self, k), self.weights[k]
-        return _ExpertLinear.apply(x, weight, _WeightUse.apply(weight, use), offsets, use)
+        use, weight, token = _Use(self, k), self.weights[k], None
+        if weight.requires_grad and torch.is_grad_enabled():
+            token = _WeightUse.apply(weight, use)
+        return _ExpertLinear.apply(x, weight, token, offsets, use)
 
     def _after_writers(self, stream, writers):
         """Work that follows on `stream` runs after the gradients' writers.  (Backward runs where

@@ -97,3 +97,23 @@ def test_only_the_weights_gradient(layer):
     units, w, x = layer
     units.linear("m", x.detach(), OFF).float().sum().backward()
     assert torch.equal(units.grads["m"], wgrad(torch.ones(8, 16), x.detach()))
+
+
+def test_checkpointed_layers_write_their_gradient_once(layer):
+    from torch.utils.checkpoint import checkpoint
+
+    units, w, x = layer
+    want = wgrad(torch.ones(8, 16), x.detach())
+    for reentrant in (False, True):
+        units.zero_grad()
+        y = checkpoint(lambda v: units.linear("m", v, OFF), x, use_reentrant=reentrant)
+        y.float().sum().backward()
+        assert torch.equal(units.grads["m"], want)
+
+
+def test_without_autograd_nothing_is_kept(layer):
+    units, w, x = layer
+    with torch.no_grad():
+        y = units.linear("m", x, OFF)
+    assert not y.requires_grad
+    assert torch.equal(y, reference(x.detach(), w.detach().as_subclass(torch.Tensor)))
