@@ -11,8 +11,8 @@ With `mask` (device bytes or bools, one per expert) only experts whose entry is
 such a call takes the tensor to write to.
 
 Argument marshalling only: everything runs in libgnmr, on torch's current stream
-of the tensors' device.  Nothing here is recorded by autograd (ExpertLinears in
-torch_experts.py does that).
+of the tensors' device.  Nothing here is recorded by autograd (ExpertUnits.linear
+in torch_experts.py is).
 """
 from __future__ import annotations
 
