@@ -27,6 +27,11 @@ def _handle(stream):
     return int(getattr(stream, "cuda_stream", stream))
 
 
+def _captured(stream):
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _FirstDerivative(torch.autograd.Function):
     """dx where backward is itself recorded: it depends on `dy` and `weight`, and whoever asks how
     is refused (the kernels that made it are not recorded)."""
@@ -147,6 +152,7 @@ class ExpertUnits:
         self._filled = [False] * len(self.weights)
         self._started = [0] * len(self.weights)     # gradients started, by matrix
         self._writers = [None] * len(self.weights)  # the stream that last wrote each
+        self._replayed = [False] * len(self.weights)    # written by a graph, unseen by the host
         U = first[-1]
         off = np.zeros(U + 1, np.int64)
         for k, w in enumerate(self.weights):
@@ -188,12 +194,14 @@ class ExpertUnits:
 
     def _after_writers(self, stream, writers):
         """Work that follows on `stream` runs after the gradients' writers.  (Backward runs where
-        forward did, on several streams perhaps; autograd orders only what passes through it.)"""
+        forward did, on several streams perhaps; autograd orders only what passes through it.)  A
+        stream under capture waits only for others of its capture, which end with it."""
         for w in {_handle(w): w for w in writers if w is not None}.values():
             if _handle(w) != _handle(stream):
                 if not hasattr(stream, "wait_stream"):
                     stream = torch.cuda.ExternalStream(_handle(stream), device=self.device)
-                stream.wait_stream(w)
+                if _captured(stream) == _captured(w):
+                    stream.wait_stream(w)
 
     def _weight_grad(self, k, dy, x, offsets):
         E, stream = self.weights[k].shape[0], self._stream(None)
@@ -202,6 +210,7 @@ class ExpertUnits:
                           accumulate=self._filled[k],
                           partials=self.partials[self._parts[k]:self._parts[k + 1]].view(E, -1))
         self._writers[k] = stream
+        self._replayed[k] |= torch.cuda.is_current_stream_capturing()
         self._started[k] += not self._filled[k]
         self._filled[k] = True
 
@@ -248,7 +257,9 @@ class OrthogonalMomentum:
     m = momentum * m + g (fp32), W -= lr * max(1, out / in)^0.5 * orthogonalize(m), all
     experts of a matrix in one call; then the units' codes are made again.  Each gradient is
     taken once: `units.step()` or `units.zero_grad()` comes between an update and the next
-    backward, else that would add to what was applied, and `step()` raises."""
+    backward, else that would add to what was applied, and `step()` raises.  (A backward that was
+    captured in a graph writes with every replay, which the host does not see: there nothing
+    is asked.)"""
 
     def __init__(self, units, lr: float, momentum: float = 0.95, steps: int = 5,
                  coefficients=ops.COEFFICIENTS, eps: float = 1e-7):
@@ -260,8 +271,9 @@ class OrthogonalMomentum:
 
     @torch.no_grad()
     def step(self) -> None:
-        for name, started, applied in zip(self.units.names, self.units._started, self._applied):
-            if started == applied:
+        for name, started, applied, replayed in zip(self.units.names, self.units._started,
+                                                    self._applied, self.units._replayed):
+            if started == applied and not replayed:
                 raise RuntimeError(f"{name}: no gradient was started since the last update")
         self._applied = list(self.units._started)
         self.units._after_writers(self.units._stream(None), self.units._writers)

@@ -78,6 +78,8 @@ def patch(monkeypatch):
     monkeypatch.setattr(E, "Controller", NotedController)
     monkeypatch.setattr(E, "_DeviceBytes", lambda ctl, n: np.zeros(n, np.uint8))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: TheStream)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
     monkeypatch.setattr(torch.cuda, "device", lambda device: contextlib.nullcontext())
     for f in (grouped_linear, grouped_dgrad, grouped_wgrad, orthogonalize):
         monkeypatch.setattr(E.ops, f.__name__, f)

@@ -77,3 +77,54 @@ def test_an_update_waits_for_the_gradients(streams, monkeypatch):
     monkeypatch.setattr(E.ops, "orthogonalize", lambda m, *a: (log.append("updates"), m)[1])
     opt.step()
     assert log == [(5, "writes"), (1, "waits for", 5), "updates"]
+
+
+@pytest.fixture
+def capture(monkeypatch, streams):
+    """Streams that are being captured."""
+    on = set()
+    current = torch.cuda.current_stream
+
+    class Under:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.stream)
+
+        def __exit__(self, *exc):
+            monkeypatch.setattr(torch.cuda, "current_stream", current)
+    monkeypatch.setattr(torch.cuda, "stream", Under)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing",
+                        lambda: torch.cuda.current_stream().cuda_stream in on)
+    return on
+
+
+def test_a_capture_does_not_wait_for_what_is_outside_it(streams, capture):
+    """Such a wait would end the capture; what came before it is its caller's to order."""
+    units, backward, log = streams
+    backward(5)                                         # a warm-up
+    units.step(1.1, 1.5, stream=Stream(5, log))
+    capture |= {6, 7}
+    backward(6)
+    backward(7)                                         # two streams of one capture
+    units.step(1.1, 1.5, stream=Stream(6, log))
+    capture.clear()
+    backward(6)
+    units.step(1.1, 1.5, stream=Stream(8, log))
+    waits = [e for e in log if "waits for" in e]
+    assert waits == [(7, "waits for", 6), (6, "waits for", 7), (6, "waits for", 7),
+                     (8, "waits for", 6)]
+
+
+def test_a_captured_gradient_is_new_with_every_replay(streams, capture):
+    """The host does not see replays, so the optimiser does not ask for a backward between them."""
+    units, backward, log = streams
+    opt = E.OrthogonalMomentum(units, lr=0.1)
+    capture.add(6)
+    backward(6)
+    capture.clear()
+    for _ in range(3):
+        opt.step()                                      # behind a replay each
+    backward(1)
+    opt.step()
