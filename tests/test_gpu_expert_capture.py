@@ -6,7 +6,8 @@ from gpu_util import require_gpu
 pytestmark = pytest.mark.gpu
 
 
-def test_forward_and_backward_captured_after_a_warm_up():
+@pytest.mark.parametrize("warm_up", ["side stream", "default stream", "earlier capture"])
+def test_forward_and_backward_captured_after_a_warm_up(warm_up):
     torch = require_gpu()
     from paper_2606_00539_amd.torch_experts import ExpertUnits, OrthogonalMomentum
 
@@ -31,12 +32,18 @@ def test_forward_and_backward_captured_after_a_warm_up():
 
     units, opt = make()
     x, dy = xs[0].clone(), dys[0].clone()
-    side = torch.cuda.Stream()
+    side = torch.cuda.Stream() if warm_up != "default stream" else torch.cuda.current_stream()
     side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):                       # the warm-up
+    with torch.cuda.stream(side):
         units.linear("m", x, off).backward(dy)
     torch.cuda.current_stream().wait_stream(side)
     units.zero_grad()
+    if warm_up == "earlier capture":
+        torch.cuda.synchronize()
+        earlier = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(earlier, stream=side):
+            units.linear("m", x, off).backward(dy)
+        units.zero_grad()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):                       # on a stream of its own
