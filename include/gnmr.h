@@ -484,6 +484,98 @@ gnmr_status gnmr_orthogonalize(const void* in, int32_t in_dtype, void* out, int3
                                int32_t cols, int32_t count, const gnmr_newton_schulz* settings,
                                void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The operators around the products of a gated block's training step: the gated
+ * feed-forward projections and their gradient, layer norm, and clipping by the
+ * global norm.  As above: asynchronous on `stream`, no allocation, nothing kept
+ * between calls, can be captured in a HIP graph; GNMR_E_INVALID (nothing launched)
+ * on a bad argument, GNMR_E_HIP on a launch failure; no output may overlap an input
+ * or another output, but for what gnmr_clip_gradients says.
+ * ------------------------------------------------------------------------- */
+enum {
+  GNMR_ACT_SILU = 0,  /* g / (1 + e^-g)                                          */
+  GNMR_ACT_GELU = 1   /* g Phi(g), Phi the normal distribution function           */
+};
+
+/* A gated feed-forward block by groups.  w: device bf16
+ * [num_groups][2 * hidden][in_features], contiguous, each group's gate matrix before its up
+ * projection; w of gnmr_gated_dgrad: the down projection's, device bf16
+ * [num_groups][out_features][hidden].  For every row t of group e, in fp32 but for the operands and
+ * one rounding of each result:
+ *   gnmr_gated_linear:      pre[t] = w_e x[t];  h[t][j] = act(pre[t][j]) pre[t][hidden + j]
+ *                           (h from the unrounded sums; pre NULL: not wanted)
+ *   gnmr_gated_activation:  h from a pre that is there
+ *   gnmr_gated_dgrad:       d[j] = sum_o dy[t][o] w_e[o][j];
+ *                           dpre[t][j] = d[j] act'(pre[t][j]) pre[t][hidden + j],
+ *                           dpre[t][hidden + j] = d[j] act(pre[t][j])
+ * The rest of the block's gradients are gnmr_grouped_dgrad of dpre and gnmr_grouped_wgrad of (dpre, x)
+ * and (dy, h).  Matrices have rows *_stride elements apart (at least their columns, a multiple of
+ * 8, below 2^22); hidden and the other features are multiples of 8, hidden below 2^21, the others
+ * below 2^22; all pointers 16-byte aligned.  Rows of no group get 0, whatever their inputs hold. */
+gnmr_status gnmr_gated_linear(const gnmr_groups* groups, const void* x, int64_t x_stride,
+                              const void* w, void* pre, int64_t pre_stride, void* h,
+                              int64_t h_stride, int32_t hidden, int32_t in_features,
+                              int32_t activation, void* stream);
+gnmr_status gnmr_gated_activation(const gnmr_groups* groups, const void* pre, int64_t pre_stride,
+                                  void* h, int64_t h_stride, int32_t hidden, int32_t activation,
+                                  void* stream);
+gnmr_status gnmr_gated_dgrad(const gnmr_groups* groups, const void* dy, int64_t dy_stride,
+                             const void* w, const void* pre, int64_t pre_stride, void* dpre,
+                             int64_t dpre_stride, int32_t out_features, int32_t hidden,
+                             int32_t activation, void* stream);
+
+/* Layer norm of each row of x, in fp32 with one rounding of y:
+ *   mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *   y = (x - mean) rstd weight + bias
+ * x, y: device, of x_dtype (GNMR_F32 or GNMR_BF16), rows *_stride elements apart (cols .. 2^28, any
+ * parity), aligned to their elements; weight, bias: device [cols] of weight_dtype, or NULL (1 and
+ * 0); mean, rstd: device float [rows], what the gradients need, or NULL.  cols 1 .. 16384, rows up
+ * to 16,777,215.  Squares of deviations have to stay below 2^128; a row with an infinity or a NaN
+ * is NaN. */
+gnmr_status gnmr_layer_norm(const void* x, int32_t x_dtype, int64_t x_stride, const void* weight,
+                            const void* bias, int32_t weight_dtype, void* y, int64_t y_stride,
+                            float* mean, float* rstd, int64_t rows, int32_t cols, float eps,
+                            void* stream);
+
+/* Its gradients, from dy (of x's type) and what the forward call left in mean and rstd:
+ *   g = dy weight, z = (x - mean) rstd;  dx = rstd (g - sum g / cols - z sum(g z) / cols),
+ *   dweight = sum over rows of dy z,  dbias = sum over rows of dy
+ * dx of x's type, dweight and dbias [cols] of weight_dtype; each may be NULL (not wanted).  The sums over
+ * rows are fp32, in an order that rows and cols fix: deterministic.  No rows give dweight and dbias 0.
+ * workspace: device, 16-byte aligned, of at least gnmr_layer_norm_backward_workspace(rows, cols)
+ * bytes; NULL where neither dweight nor dbias is wanted. */
+int64_t gnmr_layer_norm_backward_workspace(int64_t rows, int32_t cols);
+gnmr_status gnmr_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x,
+                                     int32_t x_dtype, int64_t x_stride, const float* mean,
+                                     const float* rstd, const void* weight, int32_t weight_dtype,
+                                     void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                                     int64_t rows, int32_t cols, void* workspace,
+                                     int64_t workspace_bytes, void* stream);
+
+/* The gradients' global norm, and the gradients scaled to at most max_norm:
+ *   n = sqrt(sum of the squares of the gradients that are not known + sum of norms[u]^2)
+ *   c = max_norm / (n + eps) where n + eps > max_norm, else 1 (NaN where n is NaN);  out = c in
+ * norms: device double [num_norms] of what is known (the controller's norms of
+ * gnmr_device_outputs, so that gradients that it has stepped from are not read again: set `known`
+ * in those).  Sums and products are in float64, in an order that the sizes fix: deterministic.
+ * norm: device double, gets n.  max_norm >= 0 (infinity: the norm alone), eps >= 0.  Gradients in
+ * place with c = 1 are not touched.  gradients: host array, read during the call; outs may overlap
+ * nothing but their own `in`, and that only in place.  workspace: device, 16-byte aligned, of
+ * at least gnmr_clip_gradients_workspace(num) bytes. */
+typedef struct {
+  const void* in;      /* device, aligned to its elements                          */
+  void* out;           /* device; equal to `in` (of one type): in place            */
+  int64_t numel;       /* >= 0; 2^44 values in all at most                         */
+  int32_t in_dtype;    /* GNMR_F32 or GNMR_BF16                                    */
+  int32_t out_dtype;   /* GNMR_F32 or GNMR_BF16 (rounded once)                     */
+  int32_t known;       /* 1: its squares are in `norms`                            */
+  int32_t reserved;
+} gnmr_gradient;
+int64_t gnmr_clip_gradients_workspace(int64_t num);
+gnmr_status gnmr_clip_gradients(const gnmr_gradient* gradients, int64_t num, const double* norms,
+                                int64_t num_norms, double max_norm, double eps, double* norm,
+                                void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* gnmr_last_error(void);
 

@@ -19,4 +19,7 @@ from .binding import (GNMR_BF16, GNMR_BUDGET_ACTIVE, GNMR_BUDGET_ADMITTED,  # no
                       gnmr_grouped_dgrad, gnmr_grouped_linear, gnmr_grouped_wgrad,
                       gnmr_grouped_wgrad_num_partials, gnmr_orthogonalize,
                       gnmr_orthogonalize_workspace, gnmr_quantize_rows, gnmr_quantized_linear,
-                      gnmr_quantized_linear_workspace, load_library)
+                      gnmr_quantized_linear_workspace, GNMR_ACT_GELU, GNMR_ACT_SILU,
+                      gnmr_clip_gradients, gnmr_clip_gradients_workspace, gnmr_gated_activation,
+                      gnmr_gated_dgrad, gnmr_gated_linear, gnmr_layer_norm,
+                      gnmr_layer_norm_backward, gnmr_layer_norm_backward_workspace, load_library)

@@ -27,6 +27,7 @@ STATUS_NAMES = {0: "GNMR_OK", -1: "GNMR_E_INVALID", -2: "GNMR_E_NOMEM", -3: "GNM
 
 GNMR_FMT_BF16, GNMR_FMT_E2M1, GNMR_FMT_E3M2, GNMR_FMT_E4M3, GNMR_FMT_E5M2, GNMR_FMT_INT8 = \
     0, 1, 2, 3, 4, 5
+GNMR_ACT_SILU, GNMR_ACT_GELU = 0, 1
 
 EXPORTED = ("gnmr_init", "gnmr_destroy", "gnmr_step", "gnmr_step_from_norms", "gnmr_sumsq",
             "gnmr_query", "gnmr_device_outputs", "gnmr_state_size", "gnmr_get_state",
@@ -37,7 +38,10 @@ EXPORTED = ("gnmr_init", "gnmr_destroy", "gnmr_step", "gnmr_step_from_norms", "g
             "gnmr_actuate_matrix", "gnmr_sumsq_noalloc", "gnmr_grouped_linear",
             "gnmr_grouped_dgrad", "gnmr_grouped_wgrad_num_partials", "gnmr_grouped_wgrad",
             "gnmr_quantize_rows", "gnmr_quantized_linear_workspace", "gnmr_quantized_linear",
-            "gnmr_orthogonalize_workspace", "gnmr_orthogonalize")
+            "gnmr_orthogonalize_workspace", "gnmr_orthogonalize", "gnmr_gated_linear",
+            "gnmr_gated_activation", "gnmr_gated_dgrad", "gnmr_layer_norm",
+            "gnmr_layer_norm_backward_workspace", "gnmr_layer_norm_backward",
+            "gnmr_clip_gradients_workspace", "gnmr_clip_gradients")
 GNMR_NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -81,6 +85,12 @@ class gnmr_groups(ctypes.Structure):
 class gnmr_newton_schulz(ctypes.Structure):
     _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float),
                 ("c", ctypes.c_float), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class gnmr_gradient(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("known", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class gnmr_stats(ctypes.Structure):
@@ -137,6 +147,13 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
         "gnmr_quantize_rows": [P, I32, I64, P, P, I64, I32, P],
         "gnmr_quantized_linear": [P, P, I64, P, P, P, P, I64, I32, I32, P, I64, P],
         "gnmr_orthogonalize": [P, I32, P, I32, I32, I32, P, P, I64, P],
+        "gnmr_gated_linear": [P, P, I64, P, P, I64, P, I64, I32, I32, I32, P],
+        "gnmr_gated_activation": [P, P, I64, P, I64, I32, I32, P],
+        "gnmr_gated_dgrad": [P, P, I64, P, P, I64, P, I64, I32, I32, I32, P],
+        "gnmr_layer_norm": [P, I32, I64, P, P, I32, P, I64, P, P, I64, I32, ctypes.c_float, P],
+        "gnmr_layer_norm_backward": [P, I64, P, I32, I64, P, P, P, I32, P, I64, P, P, I64, I32, P,
+                                     I64, P],
+        "gnmr_clip_gradients": [P, I64, P, I64, D, D, P, P, I64, P],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -150,6 +167,10 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
     lib.gnmr_quantized_linear_workspace.restype = I64
     lib.gnmr_orthogonalize_workspace.argtypes = [I32, I32, I32]
     lib.gnmr_orthogonalize_workspace.restype = I64
+    lib.gnmr_layer_norm_backward_workspace.argtypes = [I64, I32]
+    lib.gnmr_layer_norm_backward_workspace.restype = I64
+    lib.gnmr_clip_gradients_workspace.argtypes = [I64]
+    lib.gnmr_clip_gradients_workspace.restype = I64
     lib.gnmr_last_error.argtypes = []
     lib.gnmr_last_error.restype = ctypes.c_char_p
     if path == _LIB_PATH:
@@ -166,6 +187,8 @@ _PER_STEP = ("gnmr_step", "gnmr_step_from_norms", "gnmr_step_from_partials", "gn
              "gnmr_wgrad_sumsq_batched")
 _EXPERT_STEP = ("gnmr_grouped_linear", "gnmr_grouped_dgrad", "gnmr_grouped_wgrad",
                 "gnmr_quantize_rows", "gnmr_quantized_linear", "gnmr_orthogonalize")
+_BLOCK_STEP = ("gnmr_gated_linear", "gnmr_gated_activation", "gnmr_gated_dgrad",
+               "gnmr_layer_norm", "gnmr_layer_norm_backward", "gnmr_clip_gradients")
 
 
 def _addresses(lib, names):
@@ -186,7 +209,7 @@ class _CtypesCalls:
 
     def __init__(self, lib):
         self._f = {}
-        self.bind(lib, _addresses(lib, _PER_STEP + _EXPERT_STEP))
+        self.bind(lib, _addresses(lib, _PER_STEP + _EXPERT_STEP + _BLOCK_STEP))
 
     def bind(self, lib, addresses):
         """Calls what is at `addresses`, with the argument types of lib's functions."""
@@ -275,6 +298,53 @@ class _CtypesCalls:
             _dptr(x), int(x_dtype), _dptr(out), int(rows), int(cols), int(count),
             ctypes.byref(z), _none_or(workspace), int(workspace_bytes), _stream(stream))
 
+    def gated_linear(self, rows, num_groups, offsets, mask, mask_value, x, x_stride, w, pre,
+                     pre_stride, h, h_stride, hidden, in_features, activation, stream):
+        return self._f["gnmr_gated_linear"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(x), int(x_stride),
+            _dptr(w), _none_or(pre), int(pre_stride), _dptr(h), int(h_stride), int(hidden),
+            int(in_features), int(activation), _stream(stream))
+
+    def gated_activation(self, rows, num_groups, offsets, mask, mask_value, pre, pre_stride, h,
+                         h_stride, hidden, activation, stream):
+        return self._f["gnmr_gated_activation"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(pre), int(pre_stride),
+            _dptr(h), int(h_stride), int(hidden), int(activation), _stream(stream))
+
+    def gated_dgrad(self, rows, num_groups, offsets, mask, mask_value, dy, dy_stride, w, pre,
+                    pre_stride, dpre, dpre_stride, out_features, hidden, activation, stream):
+        return self._f["gnmr_gated_dgrad"](
+            _groups(rows, num_groups, offsets, mask, mask_value), _dptr(dy), int(dy_stride),
+            _dptr(w), _dptr(pre), int(pre_stride), _dptr(dpre), int(dpre_stride),
+            int(out_features), int(hidden), int(activation), _stream(stream))
+
+    def layer_norm(self, x, x_dtype, x_stride, weight, bias, weight_dtype, y, y_stride, mean, rstd,
+                   rows, cols, eps, stream):
+        return self._f["gnmr_layer_norm"](
+            _dptr(x), int(x_dtype), int(x_stride), _none_or(weight), _none_or(bias),
+            int(weight_dtype), _dptr(y), int(y_stride), _none_or(mean), _none_or(rstd), int(rows),
+            int(cols), float(eps), _stream(stream))
+
+    def layer_norm_backward(self, dy, dy_stride, x, x_dtype, x_stride, mean, rstd, weight,
+                            weight_dtype, dx, dx_stride, dweight, dbias, rows, cols, workspace,
+                            workspace_bytes, stream):
+        return self._f["gnmr_layer_norm_backward"](
+            _dptr(dy), int(dy_stride), _dptr(x), int(x_dtype), int(x_stride), _dptr(mean),
+            _dptr(rstd), _none_or(weight), int(weight_dtype), _none_or(dx), int(dx_stride),
+            _none_or(dweight), _none_or(dbias), int(rows), int(cols), _none_or(workspace),
+            int(workspace_bytes), _stream(stream))
+
+    def clip_gradients(self, gradients, norms, num_norms, max_norm, eps, norm, workspace,
+                       workspace_bytes, stream):
+        gs = []
+        for g, o, n, g_type, o_type, known in gradients:
+            gs.append(gnmr_gradient(_dptr(g), _dptr(o), int(n), int(g_type), int(o_type),
+                                    int(known), 0))
+        arr = (gnmr_gradient * max(len(gs), 1))(*gs)
+        return self._f["gnmr_clip_gradients"](
+            arr, len(gs), _none_or(norms), int(num_norms), float(max_norm), float(eps),
+            _dptr(norm), _none_or(workspace), int(workspace_bytes), _stream(stream))
+
 
 def _load_calls(lib):
     """The module of the per-step calls, set to the functions of `lib`."""
@@ -286,6 +356,7 @@ def _load_calls(lib):
         return _CtypesCalls(lib)
     calls.bind(_addresses(lib, _PER_STEP))
     calls.bind_experts(_addresses(lib, _EXPERT_STEP))
+    calls.bind_block(_addresses(lib, _BLOCK_STEP))
     return calls
 
 
@@ -543,6 +614,61 @@ def gnmr_orthogonalize(x, x_dtype, out, rows, cols, count, steps, coefficients, 
     a, b, c = coefficients
     _check(_native().orthogonalize(x, x_dtype, out, rows, cols, count, steps, a, b, c, eps, scale,
                                    workspace, workspace_bytes, stream))
+
+
+# -- a gated block's operators -------------------------------------------------
+# offsets, mask and mask_value as above.
+
+def gnmr_gated_linear(x, x_stride, w, pre, pre_stride, h, h_stride, rows, num_groups, hidden,
+                      in_features, activation=GNMR_ACT_SILU, offsets=None, mask=None,
+                      mask_value=1, stream=None) -> None:
+    _check(_native().gated_linear(rows, num_groups, offsets, mask, mask_value, x, x_stride, w,
+                                  pre, pre_stride, h, h_stride, hidden, in_features, activation,
+                                  stream))
+
+
+def gnmr_gated_activation(pre, pre_stride, h, h_stride, rows, num_groups, hidden,
+                          activation=GNMR_ACT_SILU, offsets=None, mask=None, mask_value=1,
+                          stream=None) -> None:
+    _check(_native().gated_activation(rows, num_groups, offsets, mask, mask_value, pre, pre_stride,
+                                      h, h_stride, hidden, activation, stream))
+
+
+def gnmr_gated_dgrad(dy, dy_stride, w, pre, pre_stride, dpre, dpre_stride, rows, num_groups,
+                     out_features, hidden, activation=GNMR_ACT_SILU, offsets=None, mask=None,
+                     mask_value=1, stream=None) -> None:
+    _check(_native().gated_dgrad(rows, num_groups, offsets, mask, mask_value, dy, dy_stride, w,
+                                 pre, pre_stride, dpre, dpre_stride, out_features, hidden,
+                                 activation, stream))
+
+
+def gnmr_layer_norm(x, x_dtype, x_stride, weight, bias, weight_dtype, y, y_stride, mean, rstd,
+                    rows, cols, eps, stream=None) -> None:
+    _check(_native().layer_norm(x, x_dtype, x_stride, weight, bias, weight_dtype, y, y_stride,
+                                mean, rstd, rows, cols, eps, stream))
+
+
+def gnmr_layer_norm_backward_workspace(rows, cols) -> int:
+    return int(load_library().gnmr_layer_norm_backward_workspace(int(rows), int(cols)))
+
+
+def gnmr_layer_norm_backward(dy, dy_stride, x, x_dtype, x_stride, mean, rstd, weight,
+                             weight_dtype, dx, dx_stride, dweight, dbias, rows, cols,
+                             workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(_native().layer_norm_backward(dy, dy_stride, x, x_dtype, x_stride, mean, rstd, weight,
+                                         weight_dtype, dx, dx_stride, dweight, dbias, rows, cols,
+                                         workspace, workspace_bytes, stream))
+
+
+def gnmr_clip_gradients_workspace(num) -> int:
+    return int(load_library().gnmr_clip_gradients_workspace(int(num)))
+
+
+def gnmr_clip_gradients(gradients, max_norm, norm, workspace, workspace_bytes, norms=None,
+                        num_norms=0, eps=1e-6, stream=None) -> None:
+    """gradients: list or tuple of (in, out, numel, in_dtype, out_dtype, known)."""
+    _check(_native().clip_gradients(gradients, norms, num_norms, max_norm, eps, norm, workspace,
+                                    workspace_bytes, stream))
 
 
 class Actuator:

@@ -255,4 +255,100 @@ int64_t orthogonal_workspace(int32_t rows, int32_t cols, int32_t count);
 hipError_t launch_orthogonal(Orthogonal a, const gnmr_newton_schulz& z, void* workspace,
                              hipStream_t s);
 
+// K9 (gated feed-forward; see k9_gated.hip)
+struct GatedLinear {
+  GroupArgs g;
+  const uint16_t* x;      // [rows][K], x_stride elements apart
+  const uint16_t* w;      // [num][2 H][K]
+  uint16_t* pre;          // [rows][2 H], pre_stride elements apart, or nullptr
+  uint16_t* h;            // [rows][H], h_stride elements apart
+  int64_t x_stride, pre_stride, h_stride;
+  int32_t H, K, tiles_n;
+  bool past;              // set by the launch: the outputs are written past the caches
+};
+struct GatedDgrad {
+  GroupArgs g;
+  const uint16_t* dy;     // [rows][K], dy_stride elements apart
+  const uint16_t* w;      // [num][K][H]
+  const uint16_t* pre;    // [rows][2 H], pre_stride elements apart
+  uint16_t* dpre;         // [rows][2 H], dpre_stride elements apart
+  int64_t dy_stride, pre_stride, dpre_stride;
+  int32_t H, K, tiles_n;
+  bool past;
+};
+struct GatedActivation {
+  GroupArgs g;
+  const uint16_t* pre;    // [rows][2 H], pre_stride elements apart
+  uint16_t* h;            // [rows][H], h_stride elements apart
+  int64_t pre_stride, h_stride;
+  int32_t H, tiles_n;
+};
+// Workgroups that the largest launch of such a call can need.
+int64_t gated_workgroups(const GroupArgs& g, int32_t hidden);
+hipError_t launch_gated_linear(const GatedLinear& a, int32_t activation, hipStream_t s);
+hipError_t launch_gated_dgrad(const GatedDgrad& a, int32_t activation, hipStream_t s);
+hipError_t launch_gated_activation(GatedActivation a, int32_t activation, hipStream_t s);
+
+// K10 (layer norm; see k10_layer_norm.hip).  Strides in elements.
+constexpr int kLayerNormCols = 16384;
+struct LayerNorm {
+  const void* x;          // [rows][cols] bf16 or fp32
+  const void *weight, *bias;  // [cols] or nullptr
+  void* y;                // [rows][cols] of x's type
+  float *mean, *rstd;     // [rows] or nullptr
+  int64_t x_stride, y_stride, rows;
+  int32_t cols;
+  float eps;
+  bool weight_f32;
+};
+struct LayerNormBackward {
+  const void *dy, *x;     // [rows][cols] bf16 or fp32
+  const float *mean, *rstd;
+  const void* weight;     // [cols] or nullptr
+  void* dx;               // [rows][cols] of x's type, or nullptr
+  void *dweight, *dbias;  // [cols] of the weight's type, or nullptr
+  float* parts;           // [num_parts][2][cols], nullptr where neither is wanted
+  int64_t dy_stride, x_stride, dx_stride, rows;
+  int32_t cols;
+  bool weight_f32;
+  int32_t num_parts;      // set by the launch
+};
+// Workgroups whose sums make the gradients of weight and bias.
+int layer_norm_parts(int64_t rows, int cols);
+hipError_t launch_layer_norm(const LayerNorm& a, bool f32, hipStream_t s);
+hipError_t launch_layer_norm_backward(LayerNormBackward a, bool f32, hipStream_t s);
+
+// K11 (clipping by the global norm; see k11_clip.hip)
+struct ClipTensor {
+  const void* in;
+  void* out;
+  int64_t numel;
+  int32_t first;          // its first chunk among those of its launch
+  uint8_t in_f32, out_f32;
+};
+constexpr int kClipTensors = 112;   // of one launch, passed by value
+struct ClipTensors {
+  int32_t num, chunks;    // tensors; their chunks of `chunk` values, the last of each ragged
+  int32_t chunk;
+  ClipTensor t[kClipTensors];
+};
+struct ClipScale {
+  const double* parts;    // [num_parts] sums of squares
+  const double* norms;    // [num_norms]
+  double* norm;           // where the global norm goes
+  double max_norm, eps;
+  int64_t num_norms;
+  int32_t num_parts;
+};
+constexpr int kClipWorkgroups = 1024;       // that sum squares in one launch, at most
+constexpr int kClipEach = 4096;             // sums and norms that every workgroup adds for itself
+constexpr int kClipLeast = 2048, kClipMost = 16384;     // values of a chunk
+constexpr int64_t kClipNumber = int64_t(1) << 20, kClipValues = int64_t(1) << 44;
+// Sums of squares of the tensors' values, one for each of `workgroups`.
+hipError_t launch_clip_squares(const ClipTensors& t, int workgroups, double* parts, hipStream_t s);
+// The sum of the parts and of the squares of the norms.
+hipError_t launch_clip_total(const ClipScale& a, double* total, hipStream_t s);
+// The global norm and the tensors scaled by what it asks for; with no tensors the norm alone.
+hipError_t launch_clip_scale(const ClipTensors& t, const ClipScale& a, hipStream_t s);
+
 }  // namespace gnmr

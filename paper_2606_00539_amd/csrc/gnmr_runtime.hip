@@ -14,6 +14,7 @@
 #include "host_call.h"
 
 using gnmr::fail;
+using gnmr::find_overlap;
 using gnmr::intersect;
 using gnmr::Item;
 using gnmr::Span;
@@ -60,10 +61,10 @@ struct DeviceGuard {
   }
 };
 
-// Index of a write that overlaps another write, or a read of a different id;
-// -1 when there is none.  O((W + R) log R): reads sorted by start, with the
-// two largest ends of distinct ids over every prefix.
-int64_t find_overlap(std::vector<Span> w, std::vector<Span> r) {
+}  // namespace
+
+// Reads sorted by start, with the two largest ends of distinct ids over every prefix.
+int64_t gnmr::find_overlap(std::vector<Span> w, std::vector<Span> r) {
   auto by_lo = [](const Span& a, const Span& b) { return a.lo < b.lo; };
   w.erase(std::remove_if(w.begin(), w.end(), [](const Span& s) { return s.lo >= s.hi; }), w.end());
   r.erase(std::remove_if(r.begin(), r.end(), [](const Span& s) { return s.lo >= s.hi; }), r.end());
@@ -106,8 +107,6 @@ int64_t find_overlap(std::vector<Span> w, std::vector<Span> r) {
   }
   return -1;
 }
-
-}  // namespace
 
 gnmr_status gnmr::fail(gnmr_status st, const std::string& msg) {
   g_last_error = msg;

@@ -277,12 +277,20 @@ inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight) {
   return r;
 }
 
+// The launches of a gated block's projections: of 2 H columns, in tiles of as many gate columns as
+// others; a 64 tile is 128 columns wide.
+inline RowLaunch gated_launch(const GroupArgs& g, int H, int K) {
+  RowLaunch r = row_launch(g, 2 * H, K, 2);
+  if (r.tile > 64) return r;
+  r.tiles_n = (H + 63) / 64;
+  r.most = most_row_tiles(g, 64) * r.tiles_n;
+  return r;
+}
+
 // Makes them: launch(edge, share, workgroups), with *tiles_n set.
 template <class Launch>
-void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* tiles_n,
-                      Launch&& launch) {
+void launch_tiles(const RowLaunch& r, int32_t* tiles_n, Launch&& launch) {
   using std::integral_constant;
-  const RowLaunch r = row_launch(g, N, K, weight);
   *tiles_n = r.tiles_n;
   const integral_constant<Share, kAll> all;
   if (r.tile == 64) return launch(integral_constant<int, 64>{}, all, r.most);
@@ -291,6 +299,11 @@ void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* til
   launch(integral_constant<int, 256>{}, integral_constant<Share, kRounds>{}, r.most);
   launch(integral_constant<int, 128>{}, integral_constant<Share, kRest>{},
          std::min<int64_t>(4 * r.most, 512));
+}
+template <class Launch>
+void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* tiles_n,
+                      Launch&& launch) {
+  launch_tiles(row_launch(g, N, K, weight), tiles_n, launch);
 }
 
 // Tile *v of group *e for workgroup w, of `num` groups with `per` tiles each.  Where a group has

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <string>
+#include <vector>
 
 #include "gnmr.h"
 
@@ -35,5 +36,9 @@ inline Span span_of(const void* p, int64_t bytes, int64_t id) {
 inline bool intersect(const Span& a, const Span& b) {
   return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
 }
+
+// Index of a write that overlaps another write, or a read of a different id;
+// -1 when there is none.  O((W + R) log R).
+int64_t find_overlap(std::vector<Span> writes, std::vector<Span> reads);
 
 }  // namespace gnmr

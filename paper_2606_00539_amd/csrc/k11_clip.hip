@@ -1,0 +1,136 @@
+// K11: the global norm of a set of gradients, and the gradients scaled to at most max_norm:
+//
+//   n = sqrt( sum over tensors of |g|^2 + sum over u of norm_u^2 ),
+//   c = max_norm / (n + eps) where n + eps > max_norm, else 1 (NaN where n is NaN);  out = c g
+//
+// norm_u are norms that are known (the controller's): their tensors need no reading for n.  Sums
+// and products are in float64, so that no gradient's square overflows or vanishes; the rate of
+// float64 on this chip is far above that of memory.  A workgroup sums the chunks w, w + G, ... of all
+// tensors; the sums are added in one order by whoever needs them, so all workgroups have the same c.
+#include "gnmr_internal.h"
+#include "lane_ops.h"
+#include "values.h"
+
+namespace gnmr {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kSweep = 8 * kThreads;    // values that a workgroup takes at a time
+
+// The tensor of chunk c, by a lane to a tensor: first[] rises, and a tensor without values
+// has the next one's first chunk.
+__device__ __forceinline__ int tensor_of(const ClipTensors& t, int c, int lane) {
+  int k = -1;
+#pragma unroll
+  for (int base = 0; base < kClipTensors; base += 64) {
+    const int i = base + lane;
+    k += __popcll(__ballot(i < t.num && t.t[i < kClipTensors ? i : 0].first <= c));
+  }
+  return k;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* red) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+template <bool kF32>
+__device__ __forceinline__ double squares(const void* p, int64_t lo, int64_t hi) {
+  double s[2] = {0.0, 0.0};
+  for (int64_t i = lo + 8 * threadIdx.x; i < hi; i += kSweep) {
+    const int64_t left = hi - i;
+    const Eight e = load_some<kF32>(p, i, left < 8 ? int(left) : 8);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s[k & 1] = fma(double(e.v[k]), double(e.v[k]), s[k & 1]);
+  }
+  return s[0] + s[1];
+}
+
+__global__ __launch_bounds__(kThreads) void k11_squares(const ClipTensors t, double* parts) {
+  __shared__ double red[4];
+  const int lane = threadIdx.x & 63;
+  double s = 0.0;
+  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const ClipTensor& k = t.t[__builtin_amdgcn_readfirstlane(tensor_of(t, c, lane))];
+    const int64_t lo = int64_t(c - k.first) * t.chunk, hi = min(lo + t.chunk, k.numel);
+    s += k.in_f32 ? squares<true>(k.in, lo, hi) : squares<false>(k.in, lo, hi);
+  }
+  s = block_sum(s, red);
+  if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+template <bool kIn, bool kOut>
+__device__ __forceinline__ void scale(const void* in, void* out, int64_t lo, int64_t hi, double c) {
+  for (int64_t i = lo + 8 * threadIdx.x; i < hi; i += kSweep) {
+    const int64_t left = hi - i;
+    const int count = left < 8 ? int(left) : 8;
+    Eight e = load_some<kIn>(in, i, count);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e.v[k] = float(double(e.v[k]) * c);
+    store_some<kOut>(out, i, count, e);
+  }
+}
+
+// This thread's share of what `threads` of them add: the parts, then the squares of the norms.
+__device__ __forceinline__ double share(const ClipScale& a, int threads) {
+  double s = 0.0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < a.num_parts; i += threads) s += a.parts[i];
+  for (int64_t i = threadIdx.x; i < a.num_norms; i += threads) s = fma(a.norms[i], a.norms[i], s);
+  return s;
+}
+
+constexpr int kTotalThreads = 1024;
+__global__ __launch_bounds__(kTotalThreads) void k11_total(const ClipScale a, double* total) {
+  __shared__ double red[kTotalThreads / 64];
+  const double s = wave_sum(share(a, kTotalThreads));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double t = 0.0;
+#pragma unroll
+  for (int i = 0; i < kTotalThreads / 64; ++i) t += red[i];
+  *total = t;
+}
+
+__global__ __launch_bounds__(kThreads) void k11_scale(const ClipTensors t, const ClipScale a) {
+  __shared__ double red[4];
+  const int lane = threadIdx.x & 63;
+  const double n = sqrt(block_sum(share(a, kThreads), red)), sum = n + a.eps;
+  const double c = sum > a.max_norm ? a.max_norm / sum : n != n ? n : 1.0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = n;
+  for (int w = blockIdx.x; w < t.chunks; w += gridDim.x) {
+    const ClipTensor& k = t.t[__builtin_amdgcn_readfirstlane(tensor_of(t, w, lane))];
+    if (c == 1.0 && k.in == k.out) continue;
+    const int64_t lo = int64_t(w - k.first) * t.chunk, hi = min(lo + t.chunk, k.numel);
+    if (k.in_f32) {
+      if (k.out_f32) scale<true, true>(k.in, k.out, lo, hi, c);
+      else scale<true, false>(k.in, k.out, lo, hi, c);
+    } else {
+      if (k.out_f32) scale<false, true>(k.in, k.out, lo, hi, c);
+      else scale<false, false>(k.in, k.out, lo, hi, c);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_clip_squares(const ClipTensors& t, int workgroups, double* parts, hipStream_t s) {
+  hipLaunchKernelGGL(k11_squares, dim3(unsigned(workgroups)), dim3(kThreads), 0, s, t, parts);
+  return hipGetLastError();
+}
+
+hipError_t launch_clip_total(const ClipScale& a, double* total, hipStream_t s) {
+  hipLaunchKernelGGL(k11_total, dim3(1), dim3(kTotalThreads), 0, s, a, total);
+  return hipGetLastError();
+}
+
+hipError_t launch_clip_scale(const ClipTensors& t, const ClipScale& a, hipStream_t s) {
+  const int most = 2 * kClipWorkgroups, wgs = t.chunks < 1 ? 1 : t.chunks < most ? t.chunks : most;
+  hipLaunchKernelGGL(k11_scale, dim3(unsigned(wgs)), dim3(kThreads), 0, s, t, a);
+  return hipGetLastError();
+}
+
+}  // namespace gnmr

@@ -1,0 +1,257 @@
+// K9: a gated feed-forward block by expert, around the products that K6 has.  Rows (tokens) lie
+// sorted by expert, expert e's in [offsets[e], offsets[e+1]); W_e has 2 H rows, the gate's first:
+//
+//   linear      p[t] = W_e x[t],  h[t][j] = act(p[t][j]) p[t][H + j]
+//   dgrad       d[t][j] = sum_o dy[t][o] V_e[o][j],
+//               dp[t][j] = d act'(p[t][j]) p[t][H + j],  dp[t][H + j] = d act(p[t][j])
+//   activation  h from a p that is there
+//
+//   silu: act(g) = g s, act'(g) = s (1 + g (1 - s)), s = 1 / (1 + e^-g)
+//   gelu: act(g) = g F, act'(g) = F + g e^(-g g / 2) / sqrt(2 pi), F = erfc(-g / sqrt 2) / 2
+//
+// bf16 operands, fp32 sums and formulas, one rounding of each result: neither p (where it is not
+// kept) nor d goes to memory.
+#include <type_traits>
+
+#include "gnmr_internal.h"
+#include "groups.h"
+#include "lane_ops.h"
+#include "mm_tile.h"
+
+namespace gnmr {
+namespace {
+
+using mm::Bf16;
+using mm::f32x4;
+using mm::u32x2;
+using mm::u32x4;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
+}
+__device__ __forceinline__ u32x2 pack(const f32x4& v) {
+  return u32x2{pack(v[0], v[1]), pack(v[2], v[3])};
+}
+__device__ __forceinline__ f32x4 four(const u32x2& v) {
+  return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u),
+               __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u)};
+}
+
+// act(g) and its derivative.  Exponential and reciprocal are the hardware's, good to a few 2^-23
+// of 1 / (1 + e^-g): a bf16 result does not see them.  They are 0 where they would lie below 2^-126
+// (g below -87, or -13 for gelu).
+struct Act {
+  float value, slope;
+};
+template <int kAct>
+__device__ __forceinline__ Act act(float g) {
+  if constexpr (kAct == GNMR_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g));
+    return Act{g * s, s * fmaf(g, 1.0f - s, 1.0f)};
+  } else {
+    // F(-u) for u >= 0 is e^(-u u / 2) times a function that falls as 1 / u: there t Q(t) with t =
+    // 1 / (1 + 0.33 u) and Q of degree 7, fitted over u up to 83 for the least relative error
+    // (1.0e-6; beyond, the exponential is 0).
+    const float e = __builtin_amdgcn_exp2f(-0.72134752f * g * g);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.33f, fabsf(g), 1.0f));
+    float q = 0.033059838f;
+    q = fmaf(q, t, -0.10479434f);
+    q = fmaf(q, t, 0.066074904f);
+    q = fmaf(q, t, 0.034522207f);
+    q = fmaf(q, t, 0.090520581f);
+    q = fmaf(q, t, 0.11733179f);
+    q = fmaf(q, t, 0.1316339f);
+    q = fmaf(q, t, 0.1316516f);
+    const float low = e * t * q, f = g < 0.0f ? low : 1.0f - low;
+    return Act{g * f, fmaf(0.39894228f * g, e, f)};
+  }
+}
+
+// Tiles of kT rows and kTN columns, kTN / 2 of gate and as many of the up projection.  (A
+// wavefront needs 64 columns for a block of each: a 64 tile is 128 wide.)
+template <int kT>
+struct GatedTile {
+  static constexpr int kTN = kT == 64 ? 128 : kT, kHidden = kTN / 2;
+  static constexpr int kStep = 128, kStages = kT == 64 ? 3 : 2, kPerCu = kT == 256 ? 1 : 2;
+  using T = mm::Tile<Bf16, false, false, kT, kTN, 2, kStep, kStages, false,
+                     mm::PairedOperand<Bf16, kTN, kStep>>;
+};
+
+template <int kAct, bool kKeep, int kT, Share kShare>
+__global__ __launch_bounds__(mm::kThreads, (GatedTile<kT>::kPerCu)) void k9_linear(
+    const GatedLinear a) {
+  using G = GatedTile<kT>;
+  using T = typename G::T;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowTile t;
+  if (!find_row_tile<kT, kShare>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  const int h0 = t.tn * G::kHidden;
+  if (kShare == kRest && h0 >= a.H) return;
+  typename T::Acc acc[T::kBM][T::kBN];
+  typename T::OpM om;
+  typename T::OpN on;
+  om.at(a.x + int64_t(t.row) * a.x_stride, a.x_stride * 2, t.rows, wave, lane);
+  const int64_t half = int64_t(a.H) * a.K;
+  const uint16_t* w = a.w + (t.group < a.g.num ? t.group * 2 * half : 0);
+  on.at(w + int64_t(h0) * a.K, half * 2, int64_t(a.K) * 2, a.H - h0, wave, lane);
+  T::product(acc, om, on, t.group < a.g.num ? a.K : 0, wave, lane);
+  if constexpr (kKeep) {
+    T::out16(
+        acc, wave, lane,
+        [](int, int, float a0, float a1, float a2, float a3) {
+          return u32x2{pack(a0, a1), pack(a2, a3)};
+        },
+        [&](int m, int n, const u32x4& v) {
+          const int j = h0 + (n >> 6) * 32 + (n & 31);
+          if (m < t.rows && j < a.H)
+            put(reinterpret_cast<u32x4*>(a.pre + int64_t(t.row + m) * a.pre_stride +
+                                         (n & 32 ? a.H : 0) + j), v, a.past);
+        });
+  }
+  T::out16_joined(
+      acc, wave, lane,
+      [](const f32x4& g, const f32x4& u) {
+        f32x4 h;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[k] = act<kAct>(g[k]).value * u[k];
+        return pack(h);
+      },
+      [&](int m, int n, const u32x4& v) {
+        if (m < t.rows && h0 + n < a.H)
+          put(reinterpret_cast<u32x4*>(a.h + int64_t(t.row + m) * a.h_stride + h0 + n), v, a.past);
+      });
+}
+
+template <int kAct, int kT, Share kShare>
+__global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, true, kT>::kPerCu)) void k9_dgrad(
+    const GatedDgrad a) {
+  using D = mm::Depth<false, true, kT>;
+  using T = mm::Tile<Bf16, false, true, kT, kT, 2, D::kStep, D::kStages>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowTile t;
+  if (!find_row_tile<kT, kShare>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  const int n0 = t.tn * kT;
+  if (kShare == kRest && n0 >= a.H) return;
+  const bool owned = t.group < a.g.num;
+  typename T::Acc acc[T::kBM][T::kBN];
+  typename T::OpM om;
+  typename T::OpN on;
+  om.at(a.dy + int64_t(t.row) * a.dy_stride, a.dy_stride * 2, t.rows, wave, lane);
+  const uint16_t* w = a.w + (owned ? int64_t(t.group) * a.H * a.K : 0);
+  on.at(w + n0, int64_t(a.H) * 2, a.H - n0, wave, lane);
+  T::product(acc, om, on, owned ? a.K : 0, wave, lane);
+  struct Pair {
+    u32x2 gate, up;
+  };
+  // (rows and columns past the last ones read those)
+  const int col = n0 + T::col(wave, lane), edge = min(col, a.H - 4);
+  T::out32(
+      acc, wave, lane,
+      [&](int q) {
+        const uint16_t* p =
+            a.pre + int64_t(t.row + min(T::row(q, wave, lane), t.rows - 1)) * a.pre_stride + edge;
+        return Pair{*reinterpret_cast<const u32x2*>(p), *reinterpret_cast<const u32x2*>(p + a.H)};
+      },
+      [&](int q, const f32x4& d, const Pair& was) {
+        const int row = T::row(q, wave, lane);
+        if (row >= t.rows || col >= a.H) return;
+        const f32x4 g = four(was.gate), u = four(was.up);
+        f32x4 dg, du;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const Act f = act<kAct>(g[k]);
+          // rows of nobody get 0, whatever their p holds
+          dg[k] = owned ? d[k] * f.slope * u[k] : 0.0f;
+          du[k] = owned ? d[k] * f.value : 0.0f;
+        }
+        uint16_t* p = a.dpre + int64_t(t.row + row) * a.dpre_stride + col;
+        put(reinterpret_cast<u32x2*>(p), pack(dg), a.past);
+        put(reinterpret_cast<u32x2*>(p + a.H), pack(du), a.past);
+      });
+}
+
+// 64 rows x 512 columns to a workgroup, eight values to a lane.
+constexpr int kActRows = 64, kActCols = 512;
+template <int kAct>
+__global__ __launch_bounds__(256) void k9_activation(const GatedActivation a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowTile t;
+  if (!find_row_tile<kActRows, kAll>(a.g, a.tiles_n, blockIdx.x, lane, &t)) return;
+  const int col = t.tn * kActCols + 8 * lane;
+  if (col >= a.H) return;
+  const bool owned = t.group < a.g.num;
+  const int rows = min(t.rows, kActRows);
+#pragma unroll 4
+  for (int r = wave; r < rows; r += 4) {
+    const uint16_t* p = a.pre + int64_t(t.row + r) * a.pre_stride + col;
+    const u32x4 g = *reinterpret_cast<const u32x4*>(p);
+    const u32x4 u = *reinterpret_cast<const u32x4*>(p + a.H);
+    u32x4 h;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const f32x4 gate = four(u32x2{g[2 * k], g[2 * k + 1]}), up = four(u32x2{u[2 * k], u[2 * k + 1]});
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = owned ? act<kAct>(gate[i]).value * up[i] : 0.0f;
+      const u32x2 two = pack(v);
+      h[2 * k] = two.x;
+      h[2 * k + 1] = two.y;
+    }
+    *reinterpret_cast<u32x4*>(a.h + int64_t(t.row + r) * a.h_stride + col) = h;
+  }
+}
+
+template <int kAct, bool kKeep>
+void launch_linear_of(GatedLinear a, hipStream_t s) {
+  a.past = past_caches(a.g.rows, int64_t(a.H) * (kKeep ? 3 : 1));
+  auto launch = [&](auto edge, auto share, int64_t wgs) {
+    hipLaunchKernelGGL((k9_linear<kAct, kKeep, decltype(edge)::value, decltype(share)::value>),
+                       dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
+  };
+  launch_tiles(gated_launch(a.g, a.H, a.K), &a.tiles_n, launch);
+}
+
+template <int kAct>
+void launch_dgrad_of(GatedDgrad a, hipStream_t s) {
+  a.past = past_caches(a.g.rows, 2 * int64_t(a.H));
+  auto launch = [&](auto edge, auto share, int64_t wgs) {
+    hipLaunchKernelGGL((k9_dgrad<kAct, decltype(edge)::value, decltype(share)::value>),
+                       dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
+  };
+  launch_row_tiles(a.g, a.H, a.K, 2, &a.tiles_n, launch);
+}
+
+}  // namespace
+
+int64_t gated_workgroups(const GroupArgs& g, int32_t hidden) {
+  return most_row_tiles(g, 64) * ((2 * int64_t(hidden) + 63) / 64);
+}
+
+hipError_t launch_gated_linear(const GatedLinear& a, int32_t activation, hipStream_t s) {
+  const bool keep = a.pre != nullptr;
+  if (activation == GNMR_ACT_SILU)
+    keep ? launch_linear_of<GNMR_ACT_SILU, true>(a, s) : launch_linear_of<GNMR_ACT_SILU, false>(a, s);
+  else
+    keep ? launch_linear_of<GNMR_ACT_GELU, true>(a, s) : launch_linear_of<GNMR_ACT_GELU, false>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_gated_dgrad(const GatedDgrad& a, int32_t activation, hipStream_t s) {
+  if (activation == GNMR_ACT_SILU) launch_dgrad_of<GNMR_ACT_SILU>(a, s);
+  else launch_dgrad_of<GNMR_ACT_GELU>(a, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_gated_activation(GatedActivation a, int32_t activation, hipStream_t s) {
+  a.tiles_n = (a.H + kActCols - 1) / kActCols;
+  const dim3 grid(unsigned(most_row_tiles(a.g, kActRows) * a.tiles_n));
+  if (activation == GNMR_ACT_SILU)
+    hipLaunchKernelGGL(k9_activation<GNMR_ACT_SILU>, grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(k9_activation<GNMR_ACT_GELU>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace gnmr

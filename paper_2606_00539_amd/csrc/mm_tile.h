@@ -142,12 +142,13 @@ struct Operand {
           off[q], 0, 0, 0);
   }
 
-  // Step s, of which only `left` values of k exist, the others zero.
-  __device__ __forceinline__ void fill(char* lds, int64_t s, int left, int wave, int lane) const {
+  // Parts [lo, hi) of step s, of which only `left` values of k exist, the others zero.
+  __device__ __forceinline__ void fill(char* lds, int64_t s, int left, int wave, int lane,
+                                       int lo = 0, int hi = kLoads) const {
     const char* p = base + s * step;
     u32x4 v[kLoads];
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) {
+    for (int q = lo; q < hi; ++q) {
       v[q] = u32x4{0, 0, 0, 0};
       const int row = (wave * kLoads + q) * kPer + lane / kChunks;
       if constexpr (kCols) {
@@ -165,8 +166,54 @@ struct Operand {
       }
     }
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q)
+    for (int q = lo; q < hi; ++q)
       *reinterpret_cast<u32x4*>(lds + (wave * kLoads + q) * 1024 + lane * 16) = v[q];
+  }
+};
+
+// A "rows" operand of kT / 2 rows of each of two matrices of one shape, in blocks of 32 by turns:
+// tile row 64 p + r is row 32 p + r of the first for r < 32, row 32 p + r - 32 of the second above.
+// What belongs together is then in the same registers of two neighbouring accumulators.
+template <class E, int kT, int kStep>
+struct PairedOperand {
+  typedef Operand<E, false, kT, kStep> Op;
+  static constexpr int kBytes = Op::kBytes, kLoads = Op::kLoads;
+  static_assert(Op::kPer <= 32, "an instruction's rows are of one matrix");
+  Op op;
+  int64_t apart;   // bytes from the first matrix to the second
+
+  static __device__ __forceinline__ int second(int q, int wave) {
+    return ((wave * Op::kLoads + q) * Op::kPer >> 5) & 1;
+  }
+
+  // `rows` of the rows exist in each matrix.
+  __device__ __forceinline__ void at(const void* p, int64_t apart_bytes, int64_t ld_bytes, int rows,
+                                     int wave, int lane) {
+    op.base = static_cast<const char*>(p);
+    op.ld = uint32_t(ld_bytes);
+    op.step = kStep;
+    apart = apart_bytes;
+#pragma unroll
+    for (int q = 0; q < Op::kLoads; ++q) {
+      const int row = (wave * Op::kLoads + q) * Op::kPer + lane / Op::kChunks;
+      const int of = (row >> 6) * 32 + (row & 31), slot = lane % Op::kChunks;
+      op.off[q] = uint32_t(of < rows ? of : rows - 1) * op.ld + 16u * (slot ^ Op::spread(row));
+    }
+  }
+
+  __device__ __forceinline__ Op of(int q, int wave) const {
+    Op o = op;
+    if (second(q, wave)) o.base += apart;
+    return o;
+  }
+  __device__ __forceinline__ void request(char* lds, int64_t s, bool there, int wave, int lo,
+                                          int hi) const {
+#pragma unroll
+    for (int q = lo; q < hi; ++q) of(q, wave).request(lds, s, there, wave, q, q + 1);
+  }
+  __device__ __forceinline__ void fill(char* lds, int64_t s, int left, int wave, int lane) const {
+#pragma unroll
+    for (int q = 0; q < Op::kLoads; ++q) of(q, wave).fill(lds, s, left, wave, lane, q, q + 1);
   }
 };
 
@@ -219,15 +266,16 @@ struct Depth {
 };
 
 // kTM x kTN tiles by kWM x (4 / kWM) wavefronts.  kSwap: accumulator registers hold
-// four rows of a column instead of four columns of a row.
+// four rows of a column instead of four columns of a row.  N: the N operand, where it is not an
+// Operand (PairedOperand).
 template <class E, bool kColsM, bool kColsN, int kTM, int kTN, int kWM, int kStep, int kStages,
-          bool kSwap = false>
+          bool kSwap = false, class N = Operand<E, kColsN, kTN, kStep>>
 struct Tile {
   static constexpr int kWN = kWaves / kWM;
   static constexpr int kWaveM = kTM / kWM, kWaveN = kTN / kWN;  // a wavefront's part
   static constexpr int kBM = kWaveM / 32, kBN = kWaveN / 32;
   typedef Operand<E, kColsM, kTM, kStep> OpM;
-  typedef Operand<E, kColsN, kTN, kStep> OpN;
+  typedef N OpN;
   static constexpr int kStepK = OpM::kStepK;
   static constexpr int kStage = OpM::kBytes + OpN::kBytes;
   typedef typename E::Acc Acc;
@@ -429,6 +477,44 @@ struct Tile {
             const Acc& a = kSwap ? acc[j][p + i] : acc[p + i][j];
             const u32x2 v = round(r0 + 32 * p + row, c0 + col, a[4 * g], a[4 * g + 1],
                                   a[4 * g + 2], a[4 * g + 3]);
+            *reinterpret_cast<u32x2*>(chunk<kRowBytes>(at, row, col / 8) + 8 * (lane >> 5)) = v;
+          }
+      lanes_meet();
+#pragma unroll 4
+      for (int r = 0; r < 32 * kPass; r += kAtOnce) {
+        const int row = r + lane / kChunks, c = lane % kChunks;
+        put(r0 + 32 * p + row, c0 + 8 * c,
+            *reinterpret_cast<const u32x4*>(chunk<kRowBytes>(at, row, c)));
+      }
+      lanes_meet();
+    }
+  }
+
+  // The same of a PairedOperand's products, a half as wide: join(a, b) makes 16-bit values (two packed
+  // words) of four of the first matrix's products and the second's, put(row, col, v) gets eight of a
+  // row at a time.
+  template <class Join, class Put>
+  static __device__ __forceinline__ void out16_joined(const Acc (&acc)[kBM][kBN], int wave, int lane,
+                                                      Join&& join, Put&& put) {
+    static_assert(!kSwap && kBN % 2 == 0, "pairs of column blocks");
+    constexpr int kRowBytes = kCols, kChunks = kRowBytes / 16, kAtOnce = 64 / kChunks;
+    constexpr int kPass = pass(kRowBytes);
+    static_assert(kRows / 32 % kPass == 0 && kPass * 32 * kRowBytes <= kRegion, "whole passes");
+    char* const at = region(wave);
+    const int r0 = first_row(wave), c0 = first_col(wave) / 2;
+    meet();
+#pragma unroll
+    for (int p = 0; p < kRows / 32; p += kPass) {
+#pragma unroll
+      for (int j = 0; j < kCols / 64; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int i = 0; i < kPass; ++i) {
+            const int row = 32 * i + (lane & 31), col = 32 * j + 8 * g + 4 * (lane >> 5);
+            const Acc &a = acc[p + i][2 * j], &b = acc[p + i][2 * j + 1];
+            const u32x2 v = join(f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]},
+                                 f32x4{b[4 * g], b[4 * g + 1], b[4 * g + 2], b[4 * g + 3]});
             *reinterpret_cast<u32x2*>(chunk<kRowBytes>(at, row, col / 8) + 8 * (lane >> 5)) = v;
           }
       lanes_meet();

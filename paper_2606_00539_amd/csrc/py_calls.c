@@ -30,9 +30,14 @@
 #define EXPERT_ENTRIES(X)                                             \
   X(gnmr_grouped_linear) X(gnmr_grouped_dgrad) X(gnmr_grouped_wgrad) \
   X(gnmr_quantize_rows) X(gnmr_quantized_linear) X(gnmr_orthogonalize)
+/* a gated block's (bind_block) */
+#define BLOCK_ENTRIES(X)                                                    \
+  X(gnmr_gated_linear) X(gnmr_gated_activation) X(gnmr_gated_dgrad)         \
+  X(gnmr_layer_norm) X(gnmr_layer_norm_backward) X(gnmr_clip_gradients)
 #define DECLARE(f) static __typeof__(&f) p_##f;
 ENTRIES(DECLARE)
 EXPERT_ENTRIES(DECLARE)
+BLOCK_ENTRIES(DECLARE)
 
 static PyObject *s_data_ptr, *s_cuda_stream, *s_value;
 
@@ -431,7 +436,134 @@ static PyObject* orthogonalize(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   return PyLong_FromLong(status);
 }
 
-/* bind({name: address}): where the entry points are; bind_experts the same of the others */
+/* -- a gated block's operators --------------------------------------------------- */
+
+static PyObject* gated_linear(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  gnmr_groups g;
+  void *x, *w, *pre, *h, *stream;
+  int64_t x_stride, pre_stride, h_stride;
+  int32_t hidden, inf, act;
+  if (arity(n, 16) || as_groups(a, &g) || as_ptr(a[5], &x) || as_i64(a[6], &x_stride) ||
+      as_ptr(a[7], &w) || as_ptr_or_null(a[8], &pre) || as_i64(a[9], &pre_stride) ||
+      as_ptr(a[10], &h) || as_i64(a[11], &h_stride) || as_i32(a[12], &hidden) ||
+      as_i32(a[13], &inf) || as_i32(a[14], &act) || as_stream(a[15], &stream))
+    return NULL;
+  CALL(p_gnmr_gated_linear(&g, x, x_stride, w, pre, pre_stride, h, h_stride, hidden, inf, act,
+                           stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* gated_activation(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  gnmr_groups g;
+  void *pre, *h, *stream;
+  int64_t pre_stride, h_stride;
+  int32_t hidden, act;
+  if (arity(n, 12) || as_groups(a, &g) || as_ptr(a[5], &pre) || as_i64(a[6], &pre_stride) ||
+      as_ptr(a[7], &h) || as_i64(a[8], &h_stride) || as_i32(a[9], &hidden) ||
+      as_i32(a[10], &act) || as_stream(a[11], &stream))
+    return NULL;
+  CALL(p_gnmr_gated_activation(&g, pre, pre_stride, h, h_stride, hidden, act, stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* gated_dgrad(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  gnmr_groups g;
+  void *dy, *w, *pre, *dpre, *stream;
+  int64_t dy_stride, pre_stride, dpre_stride;
+  int32_t outf, hidden, act;
+  if (arity(n, 16) || as_groups(a, &g) || as_ptr(a[5], &dy) || as_i64(a[6], &dy_stride) ||
+      as_ptr(a[7], &w) || as_ptr(a[8], &pre) || as_i64(a[9], &pre_stride) ||
+      as_ptr(a[10], &dpre) || as_i64(a[11], &dpre_stride) || as_i32(a[12], &outf) ||
+      as_i32(a[13], &hidden) || as_i32(a[14], &act) || as_stream(a[15], &stream))
+    return NULL;
+  CALL(p_gnmr_gated_dgrad(&g, dy, dy_stride, w, pre, pre_stride, dpre, dpre_stride, outf, hidden,
+                          act, stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* layer_norm(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *x, *weight, *bias, *y, *mean, *rstd, *stream;
+  int64_t x_stride, y_stride, rows;
+  int32_t dtype, weight_dtype, cols;
+  double eps;
+  if (arity(n, 14) || as_ptr(a[0], &x) || as_i32(a[1], &dtype) || as_i64(a[2], &x_stride) ||
+      as_ptr_or_null(a[3], &weight) || as_ptr_or_null(a[4], &bias) ||
+      as_i32(a[5], &weight_dtype) || as_ptr(a[6], &y) || as_i64(a[7], &y_stride) ||
+      as_ptr_or_null(a[8], &mean) || as_ptr_or_null(a[9], &rstd) || as_i64(a[10], &rows) ||
+      as_i32(a[11], &cols) || as_f64(a[12], &eps) || as_stream(a[13], &stream))
+    return NULL;
+  CALL(p_gnmr_layer_norm(x, dtype, x_stride, weight, bias, weight_dtype, y, y_stride, mean, rstd,
+                         rows, cols, (float)eps, stream))
+  return PyLong_FromLong(status);
+}
+
+static PyObject* layer_norm_backward(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *dy, *x, *mean, *rstd, *weight, *dx, *dweight, *dbias, *work, *stream;
+  int64_t dy_stride, x_stride, dx_stride, rows, bytes;
+  int32_t dtype, weight_dtype, cols;
+  if (arity(n, 18) || as_ptr(a[0], &dy) || as_i64(a[1], &dy_stride) || as_ptr(a[2], &x) ||
+      as_i32(a[3], &dtype) || as_i64(a[4], &x_stride) || as_ptr(a[5], &mean) ||
+      as_ptr(a[6], &rstd) || as_ptr_or_null(a[7], &weight) || as_i32(a[8], &weight_dtype) ||
+      as_ptr_or_null(a[9], &dx) || as_i64(a[10], &dx_stride) ||
+      as_ptr_or_null(a[11], &dweight) || as_ptr_or_null(a[12], &dbias) ||
+      as_i64(a[13], &rows) || as_i32(a[14], &cols) || as_ptr_or_null(a[15], &work) ||
+      as_i64(a[16], &bytes) || as_stream(a[17], &stream))
+    return NULL;
+  CALL(p_gnmr_layer_norm_backward(dy, dy_stride, x, dtype, x_stride, mean, rstd, weight,
+                                  weight_dtype, dx, dx_stride, dweight, dbias, rows, cols, work,
+                                  bytes, stream))
+  return PyLong_FromLong(status);
+}
+
+/* (in, out, numel, in_dtype, out_dtype, known) */
+static int as_gradient(PyObject* o, gnmr_gradient* g) {
+  PyObject* t = PySequence_Tuple(o);
+  if (!t) return -1;
+  int bad = -1;
+  g->reserved = 0;
+  if (PyTuple_GET_SIZE(t) != 6) {
+    PyErr_Format(PyExc_ValueError, "a gradient has 6 entries, not %zd", PyTuple_GET_SIZE(t));
+  } else if (!as_ptr(PyTuple_GET_ITEM(t, 0), (void**)&g->in) &&
+             !as_ptr(PyTuple_GET_ITEM(t, 1), &g->out) &&
+             !as_i64(PyTuple_GET_ITEM(t, 2), &g->numel) &&
+             !as_i32(PyTuple_GET_ITEM(t, 3), &g->in_dtype) &&
+             !as_i32(PyTuple_GET_ITEM(t, 4), &g->out_dtype) &&
+             !as_i32(PyTuple_GET_ITEM(t, 5), &g->known)) {
+    bad = 0;
+  }
+  Py_DECREF(t);
+  return bad;
+}
+
+static PyObject* clip_gradients(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  void *norms, *norm, *work, *stream;
+  int64_t num_norms, bytes;
+  double max_norm, eps;
+  if (arity(n, 9)) return NULL;
+  PyObject* t = PySequence_Tuple(a[0]);
+  if (!t) return NULL;
+  const Py_ssize_t count = PyTuple_GET_SIZE(t);
+  gnmr_gradient* gs = malloc((size_t)(count ? count : 1) * sizeof *gs);
+  if (!gs) {
+    Py_DECREF(t);
+    return PyErr_NoMemory();
+  }
+  int bad = 0;
+  for (Py_ssize_t i = 0; i < count && !bad; ++i) bad = as_gradient(PyTuple_GET_ITEM(t, i), gs + i);
+  Py_DECREF(t);
+  if (bad || as_ptr_or_null(a[1], &norms) || as_i64(a[2], &num_norms) ||
+      as_f64(a[3], &max_norm) || as_f64(a[4], &eps) || as_ptr(a[5], &norm) ||
+      as_ptr_or_null(a[6], &work) || as_i64(a[7], &bytes) || as_stream(a[8], &stream)) {
+    free(gs);
+    return NULL;
+  }
+  CALL(p_gnmr_clip_gradients(gs, (int64_t)count, norms, num_norms, max_norm, eps, norm, work, bytes,
+                             stream))
+  free(gs);
+  return PyLong_FromLong(status);
+}
+
+/* bind({name: address}): where the entry points are; bind_experts and bind_block the same of the others */
 static int is_dict(PyObject* const* a, Py_ssize_t n) {
   if (n == 1 && PyDict_Check(a[0])) return 1;
   PyErr_SetString(PyExc_TypeError, "bind() takes a dict of addresses");
@@ -463,6 +595,13 @@ static PyObject* bind_experts(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+static PyObject* bind_block(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  if (!is_dict(a, n)) return NULL;
+  BLOCK_ENTRIES(ADDRESS)
+  BLOCK_ENTRIES(STORE)
+  Py_RETURN_NONE;
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef kMethods[] = {METHOD(bind),
                                  METHOD(step),
@@ -480,6 +619,13 @@ static PyMethodDef kMethods[] = {METHOD(bind),
                                  METHOD(quantize_rows),
                                  METHOD(quantized_linear),
                                  METHOD(orthogonalize),
+                                 METHOD(bind_block),
+                                 METHOD(gated_linear),
+                                 METHOD(gated_activation),
+                                 METHOD(gated_dgrad),
+                                 METHOD(layer_norm),
+                                 METHOD(layer_norm_backward),
+                                 METHOD(clip_gradients),
                                  {NULL, NULL, 0, NULL}};
 static struct PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", NULL, -1, kMethods,
                                      NULL, NULL, NULL, NULL};

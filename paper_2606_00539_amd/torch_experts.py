@@ -1,6 +1,7 @@
 """A mixture-of-experts layer's matrices as GNMR units, end to end on the expert
-step's kernels: products grouped by expert, the low-cost path in INT8, weight
-gradients with the controller's sums of squares, orthogonalised updates.
+step's kernels: products grouped by expert, gated feed-forward blocks, the low-cost path
+in INT8, weight gradients with the controller's sums of squares, clipping by its norms,
+orthogonalised updates.
 
 Argument marshalling and bookkeeping only: the products, the codes, the norms and
 the updates run in libgnmr.
@@ -12,6 +13,7 @@ import torch
 
 from . import torch_ops as ops
 from .binding import GNMR_BUDGET_ACTIVE, Controller, gnmr_grouped_wgrad_num_partials
+from .torch_units import clip_from_controller
 
 
 def _readable(dy):
@@ -33,16 +35,17 @@ def _captured(stream):
 
 
 class _FirstDerivative(torch.autograd.Function):
-    """dx where backward is itself recorded: it depends on `dy` and `weight`, and whoever asks how
-    is refused (the kernels that made it are not recorded)."""
+    """dx where backward is itself recorded: it depends on `on`, and whoever asks how is refused
+    (the kernels that made it are not recorded)."""
 
     @staticmethod
-    def forward(ctx, dx, dy, weight):
+    def forward(ctx, dx, name, *on):
+        ctx.name = name
         return dx.view_as(dx)
 
     @staticmethod
     def backward(ctx, g):
-        raise RuntimeError("ExpertUnits.linear has no second derivatives")
+        raise RuntimeError(f"ExpertUnits.{ctx.name} has no second derivatives")
 
 
 class _Use:
@@ -55,6 +58,33 @@ class _Use:
     def write(self):
         rows, self.rows = self.rows, None
         self.units._weight_grad(self.k, *rows)
+
+    def product(self, x, weight, offsets):
+        """W_e x[t], each expert on its path."""
+        units, k = self.units, self.k
+        if units.codes[k] is None:
+            return ops.grouped_linear(x, weight, offsets)
+        y = torch.empty(x.shape[0], weight.shape[1], dtype=x.dtype, device=x.device)
+        mask = units.mask(k)
+        ops.grouped_linear(x, weight, offsets, mask=mask, mask_value=1, out=y)
+        ops.quantized_linear(x, *units.codes[k], offsets, mask=mask, mask_value=0, out=y)
+        return y
+
+    def gated(self, x, weight, offsets, activation, keep):
+        """(h, pre) of a gated block, each expert on its path; pre None where it is not kept."""
+        units, k = self.units, self.k
+        if units.codes[k] is None:
+            out = ops.gated_linear(x, weight, offsets, activation=activation, keep=keep)
+            return out if keep else (out, None)
+        both = weight.shape[1]
+        h = torch.empty(x.shape[0], both // 2, dtype=x.dtype, device=x.device)
+        pre = torch.empty(x.shape[0], both, dtype=x.dtype, device=x.device)
+        mask = units.mask(k)
+        ops.gated_linear(x, weight, offsets, mask=mask, mask_value=1, activation=activation, out=h,
+                         pre=pre)
+        ops.quantized_linear(x, *units.codes[k], offsets, mask=mask, mask_value=0, out=pre)
+        ops.gated_activation(pre, offsets, mask=mask, mask_value=0, activation=activation, out=h)
+        return h, pre
 
 
 class _WeightUse(torch.autograd.Function):
@@ -81,14 +111,7 @@ class _ExpertLinear(torch.autograd.Function):
     def forward(ctx, x, weight, token, offsets, use):
         ctx.save_for_backward(x, weight, offsets)
         ctx.use = use
-        units, k = use.units, use.k
-        if units.codes[k] is None:
-            return ops.grouped_linear(x, weight, offsets)
-        y = torch.empty(x.shape[0], weight.shape[1], dtype=x.dtype, device=x.device)
-        mask = units.mask(k)
-        ops.grouped_linear(x, weight, offsets, mask=mask, mask_value=1, out=y)
-        ops.quantized_linear(x, *units.codes[k], offsets, mask=mask, mask_value=0, out=y)
-        return y
+        return use.product(x, weight, offsets)
 
     @staticmethod
     def backward(ctx, dy):
@@ -98,8 +121,41 @@ class _ExpertLinear(torch.autograd.Function):
         if ctx.needs_input_grad[2]:
             ctx.use.rows, token = (rows, x, offsets), rows.new_empty(0)
         if dx is not None and torch.is_grad_enabled():      # create_graph
-            dx = _FirstDerivative.apply(dx, dy, weight)
+            dx = _FirstDerivative.apply(dx, "linear", dy, weight)
         return dx, None, token, None, None
+
+
+class _ExpertFeedForward(torch.autograd.Function):
+    """y[t] = V_e (act(G_e x[t]) * (U_e x[t])), both matrices each on its expert's path.  Backward
+    takes the products with the bf16 weights, and the derivatives at the products that
+    forward had (a straight-through gradient)."""
+
+    @staticmethod
+    def forward(ctx, x, up, down, up_token, down_token, offsets, up_use, down_use, activation,
+                keep):
+        h, pre = up_use.gated(x, up, offsets, activation, keep)
+        if keep:
+            ctx.save_for_backward(x, up, down, offsets, h, pre)
+        ctx.uses, ctx.activation = (up_use, down_use), activation
+        return down_use.product(h, down, offsets)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, up, down, offsets, h, pre = ctx.saved_tensors
+        up_use, down_use = ctx.uses
+        of_x, _, _, of_up, of_down = ctx.needs_input_grad[:5]
+        rows, dx, tokens = _readable(dy.detach()), None, [None, None]
+        if of_x or of_up:
+            dpre = ops.gated_dgrad(rows, down, pre, offsets, activation=ctx.activation)
+        if of_x:
+            dx = ops.grouped_dgrad(dpre, up, offsets)
+            if torch.is_grad_enabled():     # create_graph
+                dx = _FirstDerivative.apply(dx, "feed_forward", dy, x, up, down)
+        if of_up:
+            up_use.rows, tokens[0] = (dpre, x, offsets), rows.new_empty(0)
+        if of_down:
+            down_use.rows, tokens[1] = (rows, h, offsets), rows.new_empty(0)
+        return dx, None, None, *tokens, None, None, None, None, None
 
 
 class ExpertUnits:
@@ -110,7 +166,9 @@ class ExpertUnits:
     [offsets[e], offsets[e + 1]) (int32, on the device; a router's output need not come
     to the host).  With low_cost, experts outside A_t run in INT8 (codes of the weights
     made by `refresh()`, which an optimiser calls after it has changed them); the
-    controller's mask is read on the device when the kernels run.
+    controller's mask is read on the device when the kernels run.  `feed_forward(up, down, x,
+    offsets)` is a gated block of two of the matrices, its gate and up projections one matrix
+    ([experts, 2 hidden, in], the gate's rows first) and so one unit per expert.
 
     Backward writes the weight gradients itself, into `grads[name]` in grad_dtype, where it is
     asked for them (`torch.autograd.grad(loss, x)` leaves them alone),
@@ -185,12 +243,31 @@ class ExpertUnits:
             self.codes = [ops.quantize_rows(w.detach(), out=c)
                           for w, c in zip(self.weights, self.codes)]
 
-    def linear(self, name, x, offsets):
+    def _use(self, name):
+        """(weight, token, use) of a matrix in a product."""
         k = self._index[name]
         use, weight, token = _Use(self, k), self.weights[k], None
         if weight.requires_grad and torch.is_grad_enabled():
             token = _WeightUse.apply(weight, use)
+        return weight, token, use
+
+    def linear(self, name, x, offsets):
+        weight, token, use = self._use(name)
         return _ExpertLinear.apply(x, weight, token, offsets, use)
+
+    def feed_forward(self, up, down, x, offsets, activation="silu"):
+        """The gated block y[t] = V_e (act(G_e x[t]) * (U_e x[t])) for the rows t of every expert e:
+        matrix `up` is [G_e; U_e], [experts, 2 hidden, in], and `down` V_e, [experts, out, hidden];
+        activation "silu" or "gelu"."""
+        a, b = self.weights[self._index[up]], self.weights[self._index[down]]
+        if a.shape[0] != b.shape[0] or a.shape[1] != 2 * b.shape[2] or b.shape[2] % 8:
+            raise ValueError(f"{up} and {down} must be [experts, 2 hidden, in] and [experts, out, "
+                             f"hidden], hidden a multiple of 8, not {tuple(a.shape)} and "
+                             f"{tuple(b.shape)}")
+        keep = torch.is_grad_enabled() and any(t.requires_grad for t in (x, a, b))
+        (a, a_token, a_use), (b, b_token, b_use) = self._use(up), self._use(down)
+        return _ExpertFeedForward.apply(x, a, b, a_token, b_token, offsets, a_use, b_use, activation,
+                                        keep)
 
     def _after_writers(self, stream, writers):
         """Work that follows on `stream` runs after the gradients' writers.  (Backward runs where
@@ -227,6 +304,16 @@ class ExpertUnits:
         self._after_writers(stream, self._writers)
         self.ctl.step_from_partials(self.partials, alpha_t, beta_t, stream)
         self._filled = [False] * len(self.weights)
+
+    def step_clipped(self, alpha_t: float, beta_t: float, max_norm: float, others=(),
+                     eps: float = 1e-6, stream=None):
+        """step(), and then the gradients, with `others` (more gradient tensors of the step), scaled in
+        place to a global norm of at most max_norm.  The units' norms are those that the step has just
+        made; only `others` are read for the norm.  Returns it (a float64 scalar on the device)."""
+        stream = self._stream(stream)
+        self.step(alpha_t, beta_t, stream)
+        return clip_from_controller(self.ctl, list(self.grads.values()), others, max_norm, eps,
+                                    stream, self.device)
 
     def query(self, stream=None) -> dict:
         out = self.ctl.query(self._stream(stream))

@@ -1,8 +1,11 @@
-"""The expert step's operators on PyTorch tensors.
+"""The expert step's and a gated block's operators on PyTorch tensors.
 
   grouped_linear, grouped_dgrad, grouped_wgrad   products grouped by expert
   quantize_rows, quantized_linear                the INT8 low-cost path
   orthogonalize                                  the Newton-Schulz update
+  gated_linear, gated_activation, gated_dgrad    gated feed-forward by expert
+  layer_norm, layer_norm_backward                layer norm of rows
+  clip_gradients                                 the global norm, and clipping by it
 
 Rows (tokens) lie sorted by expert: expert e has rows [offsets[e], offsets[e + 1])
 of int32 device `offsets`; rows from offsets[-1] on belong to nobody and give 0.
@@ -11,8 +14,8 @@ With `mask` (device bytes or bools, one per expert) only experts whose entry is
 such a call takes the tensor to write to.
 
 Argument marshalling only: everything runs in libgnmr, on torch's current stream
-of the tensors' device.  Nothing here is recorded by autograd (ExpertUnits.linear
-in torch_experts.py is).
+of the tensors' device.  Nothing here is recorded by autograd (ExpertUnits.linear and
+.feed_forward in torch_experts.py and LayerNorm in torch_layers.py are).
 """
 from __future__ import annotations
 
@@ -24,6 +27,7 @@ from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.GNMR_BF16, torch.float32: B.GNMR_F32}
 _num_partials = functools.lru_cache(None)(B.gnmr_grouped_wgrad_num_partials)
+_ACTIVATIONS = {"silu": B.GNMR_ACT_SILU, "gelu": B.GNMR_ACT_GELU}
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
@@ -244,3 +248,202 @@ def orthogonalize(x, steps=5, coefficients=COEFFICIENTS, eps=1e-7, scale=1.0, ou
         B.gnmr_orthogonalize(x, _DTYPES[x.dtype], out, m, n, count, steps, coefficients, eps,
                              scale, work, size, stream)
     return out
+
+
+def _activation(name):
+    if name not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(_ACTIVATIONS)}, not {name!r}")
+    return _ACTIVATIONS[name]
+
+
+def gated_linear(x, w, offsets=None, mask=None, mask_value=1, activation="silu", keep=False,
+                 out=None, pre=None):
+    """h[t] = act(G_e x[t]) * (U_e x[t]) for the rows t of every expert e.  x: bf16 [rows, in], w:
+    bf16 [experts, 2 hidden, in], each expert's gate G_e above its U_e; activation "silu" or
+    "gelu" (by the normal distribution function); returns bf16 [rows, hidden].  With keep (or pre to
+    write them to) also the products that gated_dgrad needs: (h, pre), pre bf16 [rows, 2 hidden]."""
+    E, two, i = _weights("w", w, torch.bfloat16).shape
+    if two % 2:
+        raise ValueError("w must have a gate row for each of the others")
+    _matrix("x", x, torch.bfloat16, i)
+    act = _activation(activation)
+    _of(E, offsets, mask, x)
+    h = _output(out, mask, x.shape[0], two // 2, x)
+    if keep or pre is not None:
+        pre = _output(pre, mask, x.shape[0], two, x)
+    _same_device(x, w, h, pre)
+    device, stream = _on(x)
+    with device:
+        B.gnmr_gated_linear(x, _stride(x), w, pre, 0 if pre is None else _stride(pre), h,
+                            _stride(h), x.shape[0], E, two // 2, i, act, offsets, mask, mask_value,
+                            stream)
+    return h if pre is None else (h, pre)
+
+
+def gated_activation(pre, offsets=None, mask=None, mask_value=1, activation="silu", out=None):
+    """h = act(pre's first half) * (its second half), for products that other operators made.  The
+    number of experts is that of offsets."""
+    _matrix("pre", pre, torch.bfloat16)
+    if pre.shape[1] % 2:
+        raise ValueError("pre must have a gate column for each of the others")
+    act = _activation(activation)
+    E = 1 if offsets is None else offsets.numel() - 1
+    _of(E, offsets, mask, pre)
+    h = _output(out, mask, pre.shape[0], pre.shape[1] // 2, pre)
+    _same_device(pre, h)
+    device, stream = _on(pre)
+    with device:
+        B.gnmr_gated_activation(pre, _stride(pre), h, _stride(h), pre.shape[0], E,
+                                pre.shape[1] // 2, act, offsets, mask, mask_value, stream)
+    return h
+
+
+def gated_dgrad(dy, w, pre, offsets=None, mask=None, mask_value=1, activation="silu", out=None):
+    """The gradient of gated_linear's products from dy, that of the block's output behind its down
+    projection w (bf16 [experts, out, hidden]): (dy W_e) times the derivatives of act(gate) * up at
+    pre.  Returns bf16 [rows, 2 hidden]: grouped_dgrad and grouped_wgrad take it on."""
+    E, o, hidden = _weights("w", w, torch.bfloat16).shape
+    _matrix("dy", dy, torch.bfloat16, o)
+    _matrix("pre", pre, torch.bfloat16, 2 * hidden)
+    if pre.shape[0] != dy.shape[0]:
+        raise ValueError("dy and pre must have the same rows")
+    act = _activation(activation)
+    _of(E, offsets, mask, dy)
+    dpre = _output(out, mask, dy.shape[0], 2 * hidden, dy)
+    _same_device(dy, w, pre, dpre)
+    device, stream = _on(dy)
+    with device:
+        B.gnmr_gated_dgrad(dy, _stride(dy), w, pre, _stride(pre), dpre, _stride(dpre),
+                           dy.shape[0], E, o, hidden, act, offsets, mask, mask_value, stream)
+    return dpre
+
+
+def _rows_of(name, t, dtype, cols):
+    """t's rows over its last dimension, at any stride, as a matrix."""
+    if t.dtype != dtype or not t.is_cuda or t.dim() < 1:
+        raise TypeError(f"{name} must be a {dtype} tensor of rows on a HIP device")
+    if t.shape[-1] != cols:
+        raise ValueError(f"{name} must have {cols} columns, not {t.shape[-1]}")
+    flat = t if t.dim() == 2 else t.reshape(-1, cols)
+    rows = flat.shape[0]
+    if (cols > 1 and flat.stride(1) != 1) or (rows > 1 and flat.stride(0) < cols):
+        flat = flat.contiguous()
+    return flat
+
+
+def _row_stride(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _vector(name, t, cols, like, dtypes):
+    if t is not None and (t.dtype not in dtypes or t.shape != (cols,) or t.device != like.device or
+                          not t.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous tensor of {cols} values on x's device, of type "
+                        f"{' or '.join(str(d) for d in dtypes)}")
+    return t
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
+    """(y, mean, rstd): layer norm over x's last dimension, y = (x - mean) rstd weight + bias, and
+    the fp32 statistics of each row that layer_norm_backward takes.  x: bf16 or fp32, any leading
+    dimensions and row strides; weight and bias: bf16 or fp32, of one type, or None."""
+    if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 1:
+        raise TypeError("x must be a bf16 or fp32 tensor of rows on a HIP device")
+    cols = x.shape[-1]
+    flat = _rows_of("x", x, x.dtype, cols)
+    _vector("weight", weight, cols, x, tuple(_DTYPES))
+    _vector("bias", bias, cols, x, tuple(_DTYPES) if weight is None else (weight.dtype,))
+    wt = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+    if out is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        y = out
+        if y.shape != x.shape or y.dtype != x.dtype or y.device != x.device or \
+                (y.dim() != 2 and not y.is_contiguous()) or \
+                (y.dim() == 2 and ((cols > 1 and y.stride(1) != 1) or
+                                   (y.shape[0] > 1 and y.stride(0) < cols))):
+            raise TypeError("out must have x's shape, type and device, and contiguous rows")
+    yflat = y if y.dim() == 2 else y.view(-1, cols)
+    rows = flat.shape[0]
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    device, stream = _on(x)
+    with device:
+        B.gnmr_layer_norm(flat, _DTYPES[x.dtype], _row_stride(flat), weight, bias, _DTYPES[wt],
+                          yflat, _row_stride(yflat), mean, rstd, rows, cols, eps, stream)
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, bias=False, input_grad=True,
+                        weight_grad=True):
+    """(dx, dweight, dbias) of layer_norm, from dy (of x's type and shape) and what it returned.
+    dweight comes with a weight, in its type; dbias where bias is asked for, in that type too, or
+    fp32 without a weight; input_grad and weight_grad False leave dx and dweight out (None)."""
+    if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 1:
+        raise TypeError("x must be a bf16 or fp32 tensor of rows on a HIP device")
+    cols = x.shape[-1]
+    if dy.shape != x.shape:
+        raise ValueError(f"dy must have x's shape {tuple(x.shape)}")
+    xs, ds = _rows_of("x", x, x.dtype, cols), _rows_of("dy", dy, x.dtype, cols)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous fp32 tensor of an entry per row")
+    _vector("weight", weight, cols, x, tuple(_DTYPES))
+    _same_device(x, dy, mean, rstd)
+    wt = torch.float32 if weight is None else weight.dtype
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if input_grad else None
+    dw = torch.empty(cols, dtype=wt, device=x.device) if weight is not None and weight_grad else None
+    db = torch.empty(cols, dtype=wt, device=x.device) if bias else None
+    rows = xs.shape[0]
+    n = 0
+    if dw is not None or db is not None:
+        n = B.gnmr_layer_norm_backward_workspace(rows, cols)
+    work = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    device, stream = _on(x)
+    with device:
+        B.gnmr_layer_norm_backward(ds, _row_stride(ds), xs, _DTYPES[x.dtype], _row_stride(xs), mean,
+                                   rstd, weight, _DTYPES[wt], dx, cols, dw, db, rows, cols, work, n,
+                                   stream)
+    return dx, dw, db
+
+
+def clip_gradients(gradients, max_norm, out=None, known=(), norms=None, eps=1e-6):
+    """The gradients' global norm (a float64 scalar on their device), and the gradients scaled by
+    min(1, max_norm / (norm + eps)): in place, or into `out`, as many bf16 or fp32 tensors of their
+    shapes.  gradients: contiguous bf16 or fp32 tensors on one device.  known: indexes of gradients
+    whose norms are among `norms` (contiguous float64 on the device; the controller's, for
+    instance), so that they need no reading for the global norm.  Where that is at most max_norm, gradients
+    in place are not touched."""
+    gradients = list(gradients)
+    outs = gradients if out is None else list(out)
+    if not gradients:
+        raise ValueError("no gradient given")
+    if len(outs) != len(gradients):
+        raise ValueError(f"out must have {len(gradients)} tensors, not {len(outs)}")
+    known, like = set(known), gradients[0]
+    if not known.issubset(range(len(gradients))):
+        raise ValueError("known must be indexes of gradients")
+    if known and norms is None:
+        raise ValueError("known gradients need norms")
+    if norms is not None and (norms.dtype != torch.float64 or not norms.is_contiguous() or
+                              norms.device != like.device):
+        raise TypeError("norms must be a contiguous float64 tensor on the gradients' device")
+    table, device = [], like.device
+    for k, (g, o) in enumerate(zip(gradients, outs)):
+        if g.dtype not in _DTYPES or not g.is_cuda or not g.is_contiguous():
+            raise TypeError(f"gradient {k} must be a contiguous bf16 or fp32 tensor on a HIP device")
+        if g.device != device:
+            raise ValueError("all gradients must be on one device")
+        if o is not g and (o.dtype not in _DTYPES or o.device != device or o.shape != g.shape or
+                           not o.is_contiguous()):
+            raise TypeError(f"out {k} must be a contiguous bf16 or fp32 tensor of its gradient's shape "
+                            "and device")
+        table.append((g, o, g.numel(), _DTYPES[g.dtype], _DTYPES[o.dtype], k in known))
+    norm = torch.empty((), dtype=torch.float64, device=device)
+    n = B.gnmr_clip_gradients_workspace(len(table))
+    work = torch.empty(n, dtype=torch.uint8, device=device)
+    context, stream = _on(like)
+    with context:
+        B.gnmr_clip_gradients(table, max_norm, norm, work, n, norms,
+                              0 if norms is None else norms.numel(), eps, stream)
+    return norm

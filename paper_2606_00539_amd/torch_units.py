@@ -31,6 +31,32 @@ def _current(stream):
     return torch.cuda.current_stream()
 
 
+class _DeviceNorms:
+    """A controller's norms as an array of device float64; it keeps the controller."""
+
+    def __init__(self, ctl):
+        self.ctl = ctl
+        self.__cuda_array_interface__ = {"shape": (ctl.num_units,), "typestr": "<f8", "version": 2,
+                                         "data": (int(ctl.device_outputs()["norm"]), False)}
+
+
+def clip_from_controller(ctl, gradients, others, max_norm, eps, stream, device):
+    """The gradients that ctl has just stepped from, which are all of its units', and `others`
+    scaled in place to a global norm of at most max_norm, on `stream`; returns the norm.  Only
+    `others` are read for it."""
+    import torch
+
+    from .torch_ops import clip_gradients
+
+    if not hasattr(stream, "wait_stream"):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)),
+                                           device=device)
+    with torch.cuda.stream(stream):
+        norms = torch.as_tensor(_DeviceNorms(ctl), device=device)
+        return clip_gradients(gradients + list(others), max_norm, known=range(len(gradients)),
+                              norms=norms, eps=eps)
+
+
 def llama_linear_units(name: str):
     """Default unit map for LLaMA-style models: each attention / SwiGLU
     projection weight is one recoverable unit (Sec. 2 operator view); other
@@ -84,6 +110,17 @@ class TorchUnits:
     def step(self, alpha_t: float, beta_t: float, stream=None) -> None:
         """One controller step over the current gradients (asynchronous)."""
         self.ctl.step(alpha_t, beta_t, seg_ptr=self.grad_pointers(), stream=_current(stream))
+
+    def step_clipped(self, alpha_t: float, beta_t: float, max_norm: float, others=(),
+                     eps: float = 1e-6, stream=None):
+        """step(), and then the units' gradients, with `others` (gradients of parameters that are no
+        unit's), scaled in place to a global norm of at most max_norm.  The units' norms are those that
+        the step has just made, so their gradients are read once less than by a norm of their own.
+        Returns the norm (a float64 scalar on the device)."""
+        stream = _current(stream)
+        self.step(alpha_t, beta_t, stream)
+        return clip_from_controller(self.ctl, [p.grad for p in self.params], others, max_norm, eps,
+                                    stream, self.params[0].device)
 
     def query(self, stream=None) -> dict:
         out = self.ctl.query(_current(stream))
@@ -272,6 +309,17 @@ class FusedWgradUnits:
                     "wrote since the last step (the layer did not run, or .grad was replaced)")
         self.ctl.step_from_partials(self.partials, alpha_t, beta_t, _current(stream))
         self._produced = [None] * len(self.modules)
+
+    def step_clipped(self, alpha_t: float, beta_t: float, max_norm: float, others=(),
+                     eps: float = 1e-6, stream=None):
+        """step(), and then the weights' gradients, with `others` (the biases', for instance), scaled in
+        place to a global norm of at most max_norm.  The weights' norms are those that the step has
+        just made: their gradients are not read for it.  Returns the norm (a float64 scalar on the
+        device)."""
+        stream = _current(stream)
+        self.step(alpha_t, beta_t, stream)
+        return clip_from_controller(self.ctl, [m.weight.grad for m in self.modules], others, max_norm,
+                                    eps, stream, self.modules[0].weight.device)
 
     def query(self, stream=None) -> dict:
         out = self.ctl.query(_current(stream))
