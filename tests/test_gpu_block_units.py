@@ -1,0 +1,393 @@
+"""ExpertUnits.feed_forward, step_clipped of the units, and a block that uses all of a gated block's
+operators: outputs by path, gradients against the formulas and against differences, norms, graphs.
+
+Tolerances (u = 2^-23): each bf16 rounding is within 2^-8 of its value, each fp32 sum of K products
+within (K + 1) u of the sum of their magnitudes; they are carried through the formulas with |silu'| <
+1.1 and |silu''| <= 0.5, and 1e-5 of a value covers the kernels' own fp32 steps."""
+import os
+import sys
+
+import numpy as np
+import pytest
+
+from gpu_util import require_gpu
+from oracle import blocks as K
+from oracle import experts as X
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+U, B16 = 2.0 ** -23, 2.0 ** -8
+D, H, O, COUNTS = 72, 136, 88, (40, 0, 77, 3)
+
+
+def setup(seed, **kw):
+    torch = require_gpu()
+    from paper_2606_00539_amd.torch_experts import ExpertUnits
+
+    rng = np.random.default_rng(seed)
+    off = np.concatenate([[0], np.cumsum(COUNTS)]).astype(np.int32)
+    rows = int(off[-1]) + 6
+
+    def normal(*shape, scale=1.0):
+        return X.bf16((scale * rng.standard_normal(shape)).astype(np.float32))
+
+    def dev(a):
+        return torch.from_numpy(a).to(torch.bfloat16).cuda()
+    x, dy = normal(rows, D), normal(rows, O, scale=1e-2)
+    up, down = normal(4, 2 * H, D, scale=D ** -0.5), normal(4, O, H, scale=H ** -0.5)
+    units = ExpertUnits([("up", torch.nn.Parameter(dev(up))),
+                         ("down", torch.nn.Parameter(dev(down)))], max_o=3, lock_len=1, **kw)
+    return torch, units, off, torch.from_numpy(off).cuda(), x, up, down, dy, dev
+
+
+def products(rows, weight, off, slack):
+    """(value, how far off it may be) of rows W_e^T, `slack` of the rows, before the rounding."""
+    out, mag = X.grouped_rows(rows, weight, off)
+    more, _ = X.grouped_rows(slack, np.abs(weight), off)
+    return out, (rows.shape[1] + 1) * U * mag + more
+
+
+def chain(x, up, down, dy, off):
+    """y, dx, dup, ddown and how far off each may be, all experts in bf16."""
+    T = (0, 2, 1)
+    zero = np.zeros_like(x)
+    pre, s_pre = products(x, up.transpose(T), off, zero)
+    s_kept = s_pre + B16 * np.abs(pre)
+    g, u = np.split(pre, 2, 1)
+    sg, su = np.split(s_pre, 2, 1)
+    act, slope = K.activation(g, "silu")
+    h = act * u
+    s_h = 1.1 * sg * (np.abs(u) + su) + np.abs(act) * su + (B16 + 1e-5) * np.abs(h)
+    y, s_y = products(h, down.transpose(T), off, s_h)
+    s_y += B16 * np.abs(y)
+    d, s_d = products(dy, down, off, np.zeros_like(dy))
+    kg, ku = np.split(s_kept, 2, 1)             # the derivatives are taken at the kept products
+    dg, du = d * slope * u, d * act
+    s_dg = s_d * 1.1 * np.abs(u) + np.abs(d) * (0.5 * kg * (np.abs(u) + ku) + 1.1 * ku) + (
+        B16 + 1e-5) * np.abs(dg) + 1e-5 * np.abs(d * u)
+    s_du = s_d * (np.abs(act) + kg) + np.abs(d) * 1.1 * kg + (B16 + 1e-5) * np.abs(du)
+    dpre, s_dpre = np.concatenate([dg, du], 1), np.concatenate([s_dg, s_du], 1)
+    dpre[off[-1]:], s_dpre[off[-1]:] = 0, 0
+    dx, s_dx = products(dpre, up, off, s_dpre)
+    s_dx += B16 * np.abs(dx)
+    n = max(np.diff(off)) + 1
+    dup, mag = X.grouped_wgrad(dpre, x, off)
+    s_up = X.grouped_wgrad(s_dpre, np.abs(x), off)[0] + n * U * mag
+    ddown, mag = X.grouped_wgrad(dy, h, off)
+    s_down = X.grouped_wgrad(np.abs(dy), s_h, off)[0] + n * U * mag
+    return (y, s_y), (dx, s_dx), (dup, s_up), (ddown, s_down)
+
+
+def host(t):
+    return t.detach().float().cpu().numpy()
+
+
+def check(got, want):
+    value, slack = want
+    bad = np.abs(host(got) - value) > slack * 1.01 + 1e-37
+    assert not bad.any(), np.argwhere(bad)[:5]
+
+
+@pytest.mark.parametrize("low_cost", [False, True])
+def test_gradients_and_accumulation(low_cost):
+    """With the low-cost path and every expert recovering: the same."""
+    torch, units, off, d_off, x, up, down, dy, dev = setup(1, low_cost=low_cost)
+    if low_cost:
+        for k in range(2):
+            units.mask(k).fill_(1)
+    xt = dev(x).requires_grad_()
+    y = units.feed_forward("up", "down", xt, d_off)
+    y.backward(dev(dy))
+    want = chain(x, up, down, dy, off)
+    check(y, want[0])
+    check(xt.grad, want[1])
+    check(units.grads["up"], want[2])
+    check(units.grads["down"], want[3])
+    one = {n: g.clone() for n, g in units.grads.items()}
+    units.feed_forward("up", "down", xt, d_off).backward(dev(dy))
+    for n, g in units.grads.items():
+        assert torch.allclose(g, 2 * one[n], rtol=1e-6, atol=0)     # the second micro-batch
+    with torch.no_grad():
+        assert torch.equal(units.feed_forward("up", "down", xt, d_off), y)
+    units.step(1.1, 1.5)        # (and the mask is the controller's)
+    sq = np.concatenate([(host(units.grads[n]).astype(np.float64) ** 2).sum((1, 2))
+                         for n in ("up", "down")])
+    np.testing.assert_allclose(units.query()["norm"], np.sqrt(sq), rtol=1e-5)
+    units.close()
+
+
+def test_each_matrix_takes_its_experts_paths():
+    torch, units, off, d_off, x, up, down, dy, dev = setup(2)
+    from paper_2606_00539_amd import torch_ops as t
+
+    xt, ut, vt = dev(x), dev(up), dev(down)
+    for a, b in (([0, 0, 0, 0], [0, 0, 0, 0]), ([1, 0, 1, 0], [0, 1, 1, 0]), ([0, 0, 0, 1],
+                                                                            [1, 1, 1, 1])):
+        ma, mb = (torch.tensor(m, dtype=torch.uint8, device="cuda") for m in (a, b))
+        units.mask(0).copy_(ma)
+        units.mask(1).copy_(mb)
+        y = units.feed_forward("up", "down", xt.clone().requires_grad_(), d_off)
+        h, pre = t.gated_linear(xt, ut, d_off, keep=True)
+        low = t.quantized_linear(xt, *t.quantize_rows(ut), d_off)
+        h_low = t.gated_activation(low, d_off)
+        for e in range(4):
+            s = slice(int(off[e]), int(off[e + 1]))
+            if not a[e]:
+                h[s], pre[s] = h_low[s], low[s]
+        want, want_low = t.grouped_linear(h, vt, d_off), t.quantized_linear(
+            h, *t.quantize_rows(vt), d_off)
+        dyt = dev(dy)
+        y.backward(dyt)
+        dpre = t.gated_dgrad(dyt, vt, pre, d_off)
+        assert torch.equal(units.grads["up"], t.grouped_wgrad(dpre, xt, d_off,
+                                                              dtype=torch.float32)[0])
+        assert torch.equal(units.grads["down"], t.grouped_wgrad(dyt, h, d_off,
+                                                                dtype=torch.float32)[0])
+        units.zero_grad()
+        for e in range(4):
+            s = slice(int(off[e]), int(off[e + 1]))
+            assert torch.equal(y[s], (want if b[e] else want_low)[s])
+        assert not y[int(off[-1]):].any()
+    units.close()
+
+
+def test_gradients_against_differences():
+    """The change of sum(y dy) over a step along the gradient of x against the gradient, up to the
+    roundings of the two outputs and the third derivative."""
+    torch, units, off, d_off, x, up, down, dy, dev = setup(3, low_cost=False)
+    xt = dev(x).requires_grad_()
+    units.feed_forward("up", "down", xt, d_off).backward(dev(dy))
+    v = np.sign(host(xt.grad).astype(np.float64))
+    h = 2.0 ** -5
+    ends = []
+    for sign in (1, -1):
+        at = X.bf16((x + sign * h * v).astype(np.float32))
+        (y, s), *_ = chain(at, up, down, dy, off)
+        got = host(units.feed_forward("up", "down", dev(at), d_off)).astype(np.float64)
+        ends.append((at, (got * dy)[:off[-1]].sum(), (s * np.abs(dy))[:off[-1]].sum()))
+    step = ends[0][0].astype(np.float64) - ends[1][0]       # what the rounding left of 2 h v
+    along = float((host(xt.grad).astype(np.float64) * step).sum())
+    want = chain(x, up, down, dy, off)[1]
+    slack = ends[0][2] + ends[1][2] + float((want[1] * np.abs(step)).sum())
+    # in float64 the same difference, with what the third derivative adds
+    f = [sum(float((K.gated(a[0][s] @ up[e].T.astype(np.float64), "silu") @ down[e].T * dy[s]).sum())
+             for e in range(4) for s in [slice(off[e], off[e + 1])]) for a in ends]
+    curve = abs(f[0] - f[1] - float((want[0] * step).sum()))
+    got = ends[0][1] - ends[1][1]
+    assert abs(got - along) < slack + curve and abs(along) > 4 * curve
+    units.close()
+
+
+def test_only_what_is_asked_for_is_written():
+    torch, units, off, d_off, x, up, down, dy, dev = setup(4, low_cost=False)
+    xt = dev(x).requires_grad_()
+    for g in units.grads.values():
+        g.fill_(7.0)
+    torch.autograd.grad(units.feed_forward("up", "down", xt, d_off).float().sum(), xt)
+    assert all(bool((g == 7.0).all()) for g in units.grads.values())
+    y = units.feed_forward("up", "down", xt, d_off)
+    torch.autograd.grad(y.float().sum(), units.weights[1], allow_unused=True)
+    assert (units.grads["up"] == 7.0).all() and not (units.grads["down"] == 7.0).all()
+    units.zero_grad()
+    # no input gradient, and frozen weights
+    units.feed_forward("up", "down", dev(x), d_off).backward(dev(dy))
+    check(units.grads["up"], chain(x, up, down, dy, off)[2])
+    for w in units.weights:
+        w.requires_grad_(False)
+    assert not units.feed_forward("up", "down", dev(x), d_off).requires_grad
+    units.close()
+
+
+@pytest.mark.parametrize("low_cost", [False, True])
+def test_forward_and_backward_in_a_graph(low_cost):
+    torch, units, off, d_off, x, up, down, dy, dev = setup(5, low_cost=low_cost)
+    xs = [dev(np.roll(x, k, axis=1)) for k in range(4)]
+    dyt, want = dev(dy), []
+    for xk in xs:
+        xk = xk.clone().requires_grad_()
+        y = units.feed_forward("up", "down", xk, d_off)
+        y.backward(dyt)
+        want.append([y.detach().clone(), xk.grad.clone(),
+                     *(g.clone() for g in units.grads.values())])
+        units.zero_grad()
+    xt = xs[0].clone().requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(units.feed_forward("up", "down", xt, d_off), xt, dyt)
+    torch.cuda.current_stream().wait_stream(side)
+    units.zero_grad()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = units.feed_forward("up", "down", xt, d_off)
+        inputs = [xt, *units.weights]
+        dx = torch.autograd.grad(y, inputs, dyt, allow_unused=True)[0]
+    for k in range(4):
+        with torch.no_grad():
+            xt.copy_(xs[k])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip([y, dx, *units.grads.values()], want[k]):
+            assert torch.equal(a, b), k
+    units.close()
+
+
+def test_refusals():
+    torch, units, off, d_off, x, up, down, dy, dev = setup(6, low_cost=False)
+    xt = dev(x).requires_grad_()
+    for f in (lambda: units.feed_forward("down", "up", xt, d_off),
+              lambda: units.feed_forward("up", "up", xt, d_off),
+              lambda: units.feed_forward("up", "down", xt, d_off, activation="relu")):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(KeyError):
+        units.feed_forward("up", "none", xt, d_off)
+    g, = torch.autograd.grad(units.feed_forward("up", "down", xt, d_off).float().sum(), xt,
+                             create_graph=True)
+    with pytest.raises(RuntimeError, match="feed_forward has no second derivatives"):
+        g.float().square().sum().backward()
+    with pytest.raises(RuntimeError, match="no gradient was written"):
+        units.zero_grad()
+        units.step_clipped(1.1, 1.5, 1.0)
+    units.close()
+
+
+# -- clipping by the controller's norms -------------------------------------------------
+
+def scaled(got, was, factor):
+    """Within a rounding to fp32 of the factor's product, and one to bf16."""
+    low = B16 if got.element_size() == 2 else 0.0
+    a, b = got.double().cpu().numpy(), was.double().cpu().numpy() * factor
+    # (the controller's norms are within 1e-5 of the sums' roots)
+    return (np.abs(a - b) <= (1e-5 + low) * np.abs(b) + 1e-37).all()
+
+
+@pytest.mark.parametrize("ratio", [0.25, 4.0])
+def test_expert_units_step_clipped(ratio):
+    torch, units, off, d_off, x, up, down, dy, dev = setup(7)
+    stream = torch.cuda.Stream()
+    for how in (None, stream, stream.cuda_stream):
+        units.feed_forward("up", "down", dev(x), d_off).backward(dev(dy))
+        extra = [torch.randn(1000, device="cuda"), torch.randn(77, device="cuda").bfloat16()]
+        was = [g.clone() for g in (*units.grads.values(), *extra)]
+        norm = float(sum(g.double().square().sum() for g in was).sqrt())
+        stream.wait_stream(torch.cuda.current_stream())
+        got = units.step_clipped(1.1, 1.5, ratio * norm, others=extra, stream=how)
+        torch.cuda.synchronize()
+        assert abs(float(got) - norm) <= 1e-5 * norm
+        sq = sum(g.double().square().sum() for g in was[:2])
+        np.testing.assert_allclose((units.query()["norm"] ** 2).sum(), float(sq), rtol=2e-5)
+        for g, w in zip((*units.grads.values(), *extra), was):
+            assert scaled(g, w, ratio) if ratio < 1 else torch.equal(g, w)
+        with pytest.raises(RuntimeError):       # the gradients of a step are clipped once
+            units.step_clipped(1.1, 1.5, 1.0)
+    units.feed_forward("up", "down", dev(x), d_off).backward(dev(dy))
+    with pytest.raises(RuntimeError):           # a unit's gradient is no other one
+        units.step_clipped(1.1, 1.5, 1.0, others=[units.grads["up"]])
+    units.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_torch_units_step_clipped(dtype):
+    torch = require_gpu()
+    from paper_2606_00539_amd.torch_units import TorchUnits
+
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    m = torch.nn.Sequential(torch.nn.Linear(72, 40), torch.nn.Linear(40, 24)).to("cuda", dt)
+    units = TorchUnits(m.named_parameters(), max_o=1, lock_len=1,
+                       unit_of=lambda n: n if n.endswith("weight") else None)
+    for k in range(3):
+        m(torch.randn(30, 72, device="cuda", dtype=dt)).square().sum().backward()
+        biases = [p.grad for n, p in m.named_parameters() if n.endswith("bias")]
+        was = [p.grad.clone() for p in m.parameters()]
+        norm = float(sum(g.double().square().sum() for g in was).sqrt())
+        got = units.step_clipped(1.1, 1.5, norm / 4, others=biases, eps=0.0)
+        assert abs(float(got) - norm) <= 1e-5 * norm
+        assert all(scaled(p.grad, w, 0.25) for p, w in zip(m.parameters(), was))
+        m.zero_grad(set_to_none=k != 1)
+    units.close()
+
+
+def test_fused_wgrad_units_step_clipped():
+    torch = require_gpu()
+    from paper_2606_00539_amd.torch_units import FusedWgradUnits
+
+    m = torch.nn.Sequential(torch.nn.Linear(72, 40), torch.nn.Linear(40, 24)).to("cuda",
+                                                                                 torch.bfloat16)
+    units = FusedWgradUnits(list(m.named_children()), max_o=1, lock_len=1)
+    m(torch.randn(30, 72, device="cuda").bfloat16()).square().sum().backward()
+    was = [p.grad.clone() for p in m.parameters()]
+    norm = float(sum(g.double().square().sum() for g in was).sqrt())
+    got = units.step_clipped(1.1, 1.5, norm / 4, others=[l.bias.grad for l in m])
+    assert abs(float(got) - norm) <= 1e-5 * norm
+    assert all(scaled(p.grad, w, 0.25) for p, w in zip(m.parameters(), was))
+    units.close()
+
+
+# -- a block ----------------------------------------------------------------------------
+
+def test_a_block_of_them_together():
+    """Layer norm, routed gated experts and the residual against torch in fp32, then a step with
+    clipping."""
+    torch = require_gpu()
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    import block_step as E
+    from paper_2606_00539_amd.torch_experts import ExpertUnits
+    from paper_2606_00539_amd.torch_layers import LayerNorm
+
+    g = torch.Generator(device="cuda").manual_seed(9)
+    w = [(torch.randn(8, 2 * E.HIDDEN, E.DIM, generator=g, device="cuda") / 16).bfloat16(),
+         (torch.randn(8, E.DIM, E.HIDDEN, generator=g, device="cuda") / 18).bfloat16()]
+    units = ExpertUnits(zip(("up", "down"), map(torch.nn.Parameter, w)), low_cost=False)
+    norm = LayerNorm(E.DIM)
+    router = torch.randn(E.DIM, E.EXPERTS, generator=g, device="cuda") / 16
+    x = torch.randn(501, E.DIM, generator=g, device="cuda").bfloat16()
+    dy = torch.randn(501, E.DIM, generator=g, device="cuda")
+    r1 = router.clone().requires_grad_()
+    x1 = x.clone().requires_grad_()
+    out = E.block(x1, norm, r1, lambda r, o: units.feed_forward("up", "down", r, o))
+    out.backward(dy)
+
+    # the same in fp32, expert by expert (the layer norm's output rounded as the block's is, so that
+    # the router chooses the same experts)
+    leaves = [t.detach().float().requires_grad_() for t in (x, router, norm.weight, norm.bias, *w)]
+    xf, rf, nw, nb, up, down = leaves
+
+    def norm32(v):
+        z = torch.nn.functional.layer_norm(v, (E.DIM,), nw, nb, 1e-5)
+        return z + (z.bfloat16().float() - z).detach()
+
+    def experts(rows, offsets):
+        o = offsets.tolist()
+        parts = []
+        for e in range(8):
+            p = rows[o[e]:o[e + 1]] @ up[e].t()
+            parts.append((torch.nn.functional.silu(p[:, :E.HIDDEN]) * p[:, E.HIDDEN:]) @ down[e].t())
+        return torch.cat(parts)
+    want = E.block(xf, norm32, rf, experts)
+    want.backward(dy)
+    # seven bf16 roundings of at most 2^-8 in a row: below 3% of the norm
+    for got, ref in ((out, want), (x1.grad, xf.grad), (r1.grad, rf.grad),
+                     (norm.weight.grad, nw.grad), (norm.bias.grad, nb.grad),
+                     (units.grads["up"], up.grad), (units.grads["down"], down.grad)):
+        assert (got.float() - ref).norm() < 7 * B16 * ref.norm()
+    others = [norm.weight.grad, norm.bias.grad, r1.grad]
+    was = [t.clone() for t in (*units.grads.values(), *others)]
+    n = units.step_clipped(1.1, 1.5, 1e-3, others=others)
+    total = sum(t.double().square().sum() for t in was).sqrt()
+    assert abs(float(n) - float(total)) < 1e-5 * float(total)
+    after = sum(t.double().square().sum() for t in (*units.grads.values(), *others)).sqrt()
+    assert abs(float(after) - 1e-3) < 2e-5 * 1e-3 + 1e-6
+    units.close()
+
+
+def test_example_runs():
+    require_gpu()
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    import block_step
+
+    losses, norms, sets = block_step.train(steps=6, seed=2, log=None)
+    assert np.isfinite(losses).all() and np.isfinite(norms).all() and min(norms) > 0
+    assert all(len(s) <= 3 for s in sets)
