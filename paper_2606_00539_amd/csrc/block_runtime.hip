@@ -227,7 +227,7 @@ gnmr_status gnmr_layer_norm(const void* x, int32_t x_dtype, int64_t x_stride, co
       return fail(GNMR_E_INVALID, "an output overlaps another buffer");
     if (rows == 0) return GNMR_OK;
     const LayerNorm a{x,        weight,   bias, y,    mean, rstd, x_stride,
-                      y_stride, rows,     cols, eps,  weight_dtype == GNMR_F32};
+                      y_stride, rows,     cols, eps,  weight_dtype == GNMR_F32, 0};
     GNMR_HIP(launch_layer_norm(a, x_dtype == GNMR_F32, static_cast<hipStream_t>(stream)));
     return GNMR_OK;
   });
@@ -275,7 +275,7 @@ gnmr_status gnmr_layer_norm_backward(const void* dy, int64_t dy_stride, const vo
                               weight,    dx,       dweight,   dbias,
                               sums ? static_cast<float*>(workspace) : nullptr,
                               dy_stride, x_stride, dx_stride, rows,
-                              cols,      weight_dtype == GNMR_F32, 0};
+                              cols,      weight_dtype == GNMR_F32, 0, 0};
     GNMR_HIP(launch_layer_norm_backward(a, x_dtype == GNMR_F32, static_cast<hipStream_t>(stream)));
     return GNMR_OK;
   });
@@ -306,32 +306,33 @@ gnmr_status gnmr_clip_gradients(const gnmr_gradient* gradients, int64_t num, con
     // (ids: the gradients' places, and behind them the others)
     std::vector<Span> out{span_of(norm, 8, num), span_of(workspace, need, num + 1)};
     std::vector<Span> in{span_of(norms, 8 * num_norms, num + 2)};
-    int64_t values = 0;
+    int64_t values = 0, written = 0;
     for (int64_t k = 0; k < num; ++k) {
       const gnmr_gradient& g = gradients[k];
-      const std::string which = "gradient " + std::to_string(k);
+      auto bad = [&](const char* what) {
+        return fail(GNMR_E_INVALID, "gradient " + std::to_string(k) + ": " + what);
+      };
       if (g.numel < 0 || g.numel > kClipValues || (values += g.numel) > kClipValues)
-        return fail(GNMR_E_INVALID, which + ": numel must be >= 0, 2^44 in all at most");
+        return bad("numel must be >= 0, 2^44 in all at most");
       if (!is_dtype(g.in_dtype) || !is_dtype(g.out_dtype))
-        return fail(GNMR_E_INVALID, which + ": types must be GNMR_F32 or GNMR_BF16");
-      if (g.known != 0 && g.known != 1)
-        return fail(GNMR_E_INVALID, which + ": known must be 0 or 1");
+        return bad("types must be GNMR_F32 or GNMR_BF16");
+      if (g.known != 0 && g.known != 1) return bad("known must be 0 or 1");
       if (g.numel > 0 && (g.in == nullptr || g.out == nullptr))
-        return fail(GNMR_E_INVALID, which + ": in and out must be device pointers");
+        return bad("in and out must be device pointers");
       const int64_t si = size_of(g.in_dtype), so = size_of(g.out_dtype);
       if (!aligned(g.in, uintptr_t(si)) || !aligned(g.out, uintptr_t(so)))
-        return fail(GNMR_E_INVALID, which + ": in and out must be aligned to their elements");
+        return bad("in and out must be aligned to their elements");
       in.push_back(span_of(g.in, g.numel * si, k));
       out.push_back(span_of(g.out, g.numel * so, k));
+      written += g.numel * so;
       if (intersect(in.back(), out.back()) && (g.in != g.out || g.in_dtype != g.out_dtype))
-        return fail(GNMR_E_INVALID, which + ": out overlaps in (in place needs the same address "
-                                            "and type)");
+        return bad("out overlaps in (in place needs the same address and type)");
     }
-    const int64_t bad = find_overlap(out, in);
-    if (bad != -1)
+    const int64_t met = find_overlap(out, in);
+    if (met != -1)
       return fail(GNMR_E_INVALID,
-                  (bad >= num ? std::string("norm or the workspace")
-                              : "gradient " + std::to_string(bad) + ": out") +
+                  (met >= num ? std::string("norm or the workspace")
+                              : "gradient " + std::to_string(met) + ": out") +
                       " overlaps another buffer");
     const hipStream_t st = static_cast<hipStream_t>(stream);
     double* const parts = static_cast<double*>(workspace) + 1;
@@ -352,7 +353,7 @@ gnmr_status gnmr_clip_gradients(const gnmr_gradient* gradients, int64_t num, con
     }
     auto scaled = clip_launches(gradients, num, [](const gnmr_gradient&) { return true; });
     if (scaled.empty()) scaled.push_back(ClipTensors{});
-    for (const ClipTensors& l : scaled) GNMR_HIP(launch_clip_scale(l, s, st));
+    for (const ClipTensors& l : scaled) GNMR_HIP(launch_clip_scale(l, s, written > kClipCached, st));
     return GNMR_OK;
   });
 }

@@ -300,6 +300,7 @@ struct LayerNorm {
   int32_t cols;
   float eps;
   bool weight_f32;
+  int32_t waves;          // set by the launch: wavefronts to a row
 };
 struct LayerNormBackward {
   const void *dy, *x;     // [rows][cols] bf16 or fp32
@@ -311,11 +312,11 @@ struct LayerNormBackward {
   int64_t dy_stride, x_stride, dx_stride, rows;
   int32_t cols;
   bool weight_f32;
-  int32_t num_parts;      // set by the launch
+  int32_t num_parts, waves;   // set by the launch
 };
 // Workgroups whose sums make the gradients of weight and bias.
 int layer_norm_parts(int64_t rows, int cols);
-hipError_t launch_layer_norm(const LayerNorm& a, bool f32, hipStream_t s);
+hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s);
 hipError_t launch_layer_norm_backward(LayerNormBackward a, bool f32, hipStream_t s);
 
 // K11 (clipping by the global norm; see k11_clip.hip)
@@ -342,6 +343,7 @@ struct ClipScale {
 };
 constexpr int kClipWorkgroups = 1024;       // that sum squares in one launch, at most
 constexpr int kClipEach = 4096;             // sums and norms that every workgroup adds for itself
+constexpr int64_t kClipCached = int64_t(32) << 20;      // bytes of outs that go through the caches
 constexpr int kClipLeast = 2048, kClipMost = 16384;     // values of a chunk
 constexpr int64_t kClipNumber = int64_t(1) << 20, kClipValues = int64_t(1) << 44;
 // Sums of squares of the tensors' values, one for each of `workgroups`.
@@ -349,6 +351,6 @@ hipError_t launch_clip_squares(const ClipTensors& t, int workgroups, double* par
 // The sum of the parts and of the squares of the norms.
 hipError_t launch_clip_total(const ClipScale& a, double* total, hipStream_t s);
 // The global norm and the tensors scaled by what it asks for; with no tensors the norm alone.
-hipError_t launch_clip_scale(const ClipTensors& t, const ClipScale& a, hipStream_t s);
+hipError_t launch_clip_scale(const ClipTensors& t, const ClipScale& a, bool past, hipStream_t s);
 
 }  // namespace gnmr

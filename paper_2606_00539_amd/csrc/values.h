@@ -6,73 +6,96 @@
 
 namespace gnmr {
 
-// Vectors that need the alignment of their elements only.
-typedef uint32_t AnyU32x4 __attribute__((ext_vector_type(4), aligned(2)));
-typedef float AnyF32x4 __attribute__((ext_vector_type(4), aligned(4)));
-
-struct Eight {
-  float v[8];
+template <int N>
+struct Run {
+  float v[N];
 };
 
-__device__ __forceinline__ float bf16_value(uint16_t bits) {
-  return __uint_as_float(uint32_t(bits) << 16);
-}
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   typedef __bf16 Two __attribute__((ext_vector_type(2)));
   typedef float F32x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(F32x2{lo, hi}, Two));
 }
 
-// The eight values from element i on.
-template <bool kF32>
-__device__ __forceinline__ Eight load_eight(const void* p, int64_t i) {
-  Eight e;
-  if constexpr (kF32) {
-    const AnyF32x4* q = reinterpret_cast<const AnyF32x4*>(static_cast<const float*>(p) + i);
-    const AnyF32x4 a = q[0], b = q[1];
+// N values (4, or 8 of bf16) as they lie in memory: one access of up to 16 bytes.
+template <bool kF32, int N>
+struct Raw {
+  static_assert(N == 4 || (N == 8 && !kF32), "16 bytes at most");
+  static constexpr int kWords = kF32 ? N : N / 2, kBytes = kF32 ? 4 : 2;
+  typedef uint32_t Words __attribute__((ext_vector_type(kWords), aligned(kBytes)));
+  uint32_t w[kWords];
+
+  __device__ __forceinline__ Run<N> values() const {
+    Run<N> e;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      e.v[k] = a[k];
-      e.v[4 + k] = b[k];
+    for (int k = 0; k < kWords; ++k) {
+      if constexpr (kF32) {
+        e.v[k] = __uint_as_float(w[k]);
+      } else {
+        e.v[2 * k] = __uint_as_float(w[k] << 16);
+        e.v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+      }
     }
-  } else {
-    const AnyU32x4 a = *reinterpret_cast<const AnyU32x4*>(static_cast<const uint16_t*>(p) + i);
+    return e;
+  }
+};
+
+// The values from element i on, through the caches or past them.
+template <bool kF32, int N, bool kPast = false>
+__device__ __forceinline__ Raw<kF32, N> load_raw(const void* p, int64_t i) {
+  typedef Raw<kF32, N> R;
+  typedef typename R::Words Words;
+  const Words* q = reinterpret_cast<const Words*>(static_cast<const char*>(p) + i * R::kBytes);
+  Words v;
+  if constexpr (kPast) v = __builtin_nontemporal_load(q);
+  else v = *q;
+  R r;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      e.v[2 * k] = __uint_as_float(a[k] << 16);
-      e.v[2 * k + 1] = __uint_as_float(a[k] & 0xFFFF0000u);
+  for (int k = 0; k < R::kWords; ++k) r.w[k] = v[k];
+  return r;
+}
+
+// `count` of them, zeros behind.
+template <bool kF32, int N>
+__device__ __forceinline__ Raw<kF32, N> load_raw_some(const void* p, int64_t i, int count) {
+  if (count >= N) return load_raw<kF32, N>(p, i);
+  Raw<kF32, N> r;
+#pragma unroll
+  for (int k = 0; k < Raw<kF32, N>::kWords; ++k) {
+    r.w[k] = 0;
+    if constexpr (kF32) {
+      if (k < count) r.w[k] = static_cast<const uint32_t*>(p)[i + k];
+    } else {
+      const uint16_t* q = static_cast<const uint16_t*>(p) + i + 2 * k;
+      if (2 * k < count) r.w[k] = q[0];
+      if (2 * k + 1 < count) r.w[k] |= uint32_t(q[1]) << 16;
     }
   }
-  return e;
+  return r;
 }
 
-template <bool kF32>
-__device__ __forceinline__ float load_one(const void* p, int64_t i) {
-  if constexpr (kF32) return static_cast<const float*>(p)[i];
-  else return bf16_value(static_cast<const uint16_t*>(p)[i]);
+template <bool kF32, int N, bool kPast = false>
+__device__ __forceinline__ Run<N> load_run(const void* p, int64_t i) {
+  return load_raw<kF32, N, kPast>(p, i).values();
+}
+template <bool kF32, int N>
+__device__ __forceinline__ Run<N> load_some(const void* p, int64_t i, int count) {
+  return load_raw_some<kF32, N>(p, i, count).values();
 }
 
-// `count` values from element i on, zeros behind them.
-template <bool kF32>
-__device__ __forceinline__ Eight load_some(const void* p, int64_t i, int count) {
-  if (count >= 8) return load_eight<kF32>(p, i);
-  Eight e;
+template <bool kF32, int N, bool kPast = false>
+__device__ __forceinline__ void store_run(void* p, int64_t i, const Run<N>& e) {
+  typedef Raw<kF32, N> R;
+  typedef typename R::Words Words;
+  Words v;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) e.v[k] = k < count ? load_one<kF32>(p, i + k) : 0.0f;
-  return e;
-}
-
-template <bool kF32>
-__device__ __forceinline__ void store_eight(void* p, int64_t i, const Eight& e) {
-  if constexpr (kF32) {
-    AnyF32x4* q = reinterpret_cast<AnyF32x4*>(static_cast<float*>(p) + i);
-    q[0] = AnyF32x4{e.v[0], e.v[1], e.v[2], e.v[3]};
-    q[1] = AnyF32x4{e.v[4], e.v[5], e.v[6], e.v[7]};
-  } else {
-    *reinterpret_cast<AnyU32x4*>(static_cast<uint16_t*>(p) + i) =
-        AnyU32x4{bf16_pair(e.v[0], e.v[1]), bf16_pair(e.v[2], e.v[3]),
-                 bf16_pair(e.v[4], e.v[5]), bf16_pair(e.v[6], e.v[7])};
+  for (int k = 0; k < R::kWords; ++k) {
+    if constexpr (kF32) v[k] = __float_as_uint(e.v[k]);
+    else v[k] = bf16_pair(e.v[2 * k], e.v[2 * k + 1]);
   }
+  Words* q = reinterpret_cast<Words*>(static_cast<char*>(p) + i * R::kBytes);
+  if constexpr (kPast) __builtin_nontemporal_store(v, q);
+  else *q = v;
 }
 
 template <bool kF32>
@@ -81,11 +104,11 @@ __device__ __forceinline__ void store_one(void* p, int64_t i, float v) {
   else static_cast<uint16_t*>(p)[i] = uint16_t(bf16_pair(v, v));
 }
 
-template <bool kF32>
-__device__ __forceinline__ void store_some(void* p, int64_t i, int count, const Eight& e) {
-  if (count >= 8) return store_eight<kF32>(p, i, e);
+template <bool kF32, int N>
+__device__ __forceinline__ void store_some(void* p, int64_t i, int count, const Run<N>& e) {
+  if (count >= N) return store_run<kF32, N>(p, i, e);
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
+  for (int k = 0; k < N; ++k)
     if (k < count) store_one<kF32>(p, i + k, e.v[k]);
 }
 
