@@ -328,11 +328,15 @@ struct ClipTensor {
   uint8_t in_f32, out_f32;
 };
 constexpr int kClipTensors = 112;   // of one launch, passed by value
-struct ClipTensors {
+constexpr int kClipFew = 30;        // the most that go in a shorter argument
+template <int kMostTensors>
+struct ClipTensorsOf {
+  static constexpr int kMost = kMostTensors;
   int32_t num, chunks;    // tensors; their chunks of `chunk` values, the last of each ragged
   int32_t chunk;
-  ClipTensor t[kClipTensors];
+  ClipTensor t[kMost];
 };
+typedef ClipTensorsOf<kClipTensors> ClipTensors;
 struct ClipScale {
   const double* parts;    // [num_parts] sums of squares
   const double* norms;    // [num_norms]

@@ -7,6 +7,8 @@
 // and products are in float64, so that no gradient's square overflows or vanishes; the rate of
 // float64 on this chip is far above that of memory.  A workgroup sums the chunks w, w + G, ... of all
 // tensors; the sums are added in one order by whoever needs them, so all workgroups have the same c.
+#include <type_traits>
+
 #include "gnmr_internal.h"
 #include "lane_ops.h"
 #include "values.h"
@@ -17,12 +19,13 @@ namespace {
 constexpr int kThreads = 256;
 // The tensor of chunk c, by a lane to a tensor: first[] rises, and a tensor without values
 // has the next one's first chunk.
-__device__ __forceinline__ int tensor_of(const ClipTensors& t, int c, int lane) {
+template <class T>
+__device__ __forceinline__ int tensor_of(const T& t, int c, int lane) {
   int k = -1;
 #pragma unroll
-  for (int base = 0; base < kClipTensors; base += 64) {
+  for (int base = 0; base < T::kMost; base += 64) {
     const int i = base + lane;
-    k += __popcll(__ballot(i < t.num && t.t[i < kClipTensors ? i : 0].first <= c));
+    k += __popcll(__ballot(i < t.num && t.t[i < T::kMost ? i : 0].first <= c));
   }
   return k;
 }
@@ -65,7 +68,8 @@ __device__ __forceinline__ double squares(const void* p, int64_t lo, int64_t hi)
   return s[0] + s[1];
 }
 
-__global__ __launch_bounds__(kThreads) void k11_squares(const ClipTensors t, double* parts) {
+template <class T>
+__global__ __launch_bounds__(kThreads) void k11_squares(const T t, double* parts) {
   __shared__ double red[4];
   const int lane = threadIdx.x & 63;
   double s = 0.0;
@@ -130,8 +134,8 @@ __global__ __launch_bounds__(kTotalThreads) void k11_total(const ClipScale a, do
   *total = t;
 }
 
-template <bool kPast>
-__global__ __launch_bounds__(kThreads) void k11_scale(const ClipTensors t, const ClipScale a) {
+template <bool kPast, class T>
+__global__ __launch_bounds__(kThreads) void k11_scale(const T t, const ClipScale a) {
   __shared__ double red[4];
   const int lane = threadIdx.x & 63;
   const double n = sqrt(block_sum(share(a, kThreads), red)), sum = n + a.eps;
@@ -153,10 +157,25 @@ __global__ __launch_bounds__(kThreads) void k11_scale(const ClipTensors t, const
   }
 }
 
+// launch(the tensors, in an argument of 1 KB where they fit one): the host copies it whole.
+template <class Launch>
+void with_few(const ClipTensors& t, Launch&& launch) {
+  if (t.num > kClipFew) return launch(t);
+  ClipTensorsOf<kClipFew> few;
+  few.num = t.num;
+  few.chunks = t.chunks;
+  few.chunk = t.chunk;
+  for (int i = 0; i < kClipFew; ++i) few.t[i] = t.t[i];
+  launch(few);
+}
+
 }  // namespace
 
 hipError_t launch_clip_squares(const ClipTensors& t, int workgroups, double* parts, hipStream_t s) {
-  hipLaunchKernelGGL(k11_squares, dim3(unsigned(workgroups)), dim3(kThreads), 0, s, t, parts);
+  with_few(t, [&](const auto& some) {
+    hipLaunchKernelGGL((k11_squares<std::decay_t<decltype(some)>>), dim3(unsigned(workgroups)),
+                       dim3(kThreads), 0, s, some, parts);
+  });
   return hipGetLastError();
 }
 
@@ -167,8 +186,12 @@ hipError_t launch_clip_total(const ClipScale& a, double* total, hipStream_t s) {
 
 hipError_t launch_clip_scale(const ClipTensors& t, const ClipScale& a, bool past, hipStream_t s) {
   const int most = 2 * kClipWorkgroups, wgs = t.chunks < 1 ? 1 : t.chunks < most ? t.chunks : most;
-  if (past) hipLaunchKernelGGL(k11_scale<true>, dim3(unsigned(wgs)), dim3(kThreads), 0, s, t, a);
-  else hipLaunchKernelGGL(k11_scale<false>, dim3(unsigned(wgs)), dim3(kThreads), 0, s, t, a);
+  with_few(t, [&](const auto& some) {
+    typedef std::decay_t<decltype(some)> T;
+    const dim3 grid{unsigned(wgs)}, block(kThreads);
+    if (past) hipLaunchKernelGGL((k11_scale<true, T>), grid, block, 0, s, some, a);
+    else hipLaunchKernelGGL((k11_scale<false, T>), grid, block, 0, s, some, a);
+  });
   return hipGetLastError();
 }
 

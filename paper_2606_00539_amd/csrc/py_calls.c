@@ -520,15 +520,19 @@ static int as_gradient(PyObject* o, gnmr_gradient* g) {
   PyObject* t = PySequence_Tuple(o);
   if (!t) return -1;
   int bad = -1;
+  void* in = NULL;
   g->reserved = 0;
   if (PyTuple_GET_SIZE(t) != 6) {
     PyErr_Format(PyExc_ValueError, "a gradient has 6 entries, not %zd", PyTuple_GET_SIZE(t));
-  } else if (!as_ptr(PyTuple_GET_ITEM(t, 0), (void**)&g->in) &&
-             !as_ptr(PyTuple_GET_ITEM(t, 1), &g->out) &&
+  } else if (!as_ptr(PyTuple_GET_ITEM(t, 0), &in) &&
+             (PyTuple_GET_ITEM(t, 1) == PyTuple_GET_ITEM(t, 0)
+                  ? (g->out = in, 0)
+                  : as_ptr(PyTuple_GET_ITEM(t, 1), &g->out)) == 0 &&
              !as_i64(PyTuple_GET_ITEM(t, 2), &g->numel) &&
              !as_i32(PyTuple_GET_ITEM(t, 3), &g->in_dtype) &&
              !as_i32(PyTuple_GET_ITEM(t, 4), &g->out_dtype) &&
              !as_i32(PyTuple_GET_ITEM(t, 5), &g->known)) {
+    g->in = in;
     bad = 0;
   }
   Py_DECREF(t);

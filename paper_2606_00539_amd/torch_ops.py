@@ -27,6 +27,7 @@ from . import binding as B
 
 _DTYPES = {torch.bfloat16: B.GNMR_BF16, torch.float32: B.GNMR_F32}
 _num_partials = functools.lru_cache(None)(B.gnmr_grouped_wgrad_num_partials)
+_clip_workspace = functools.lru_cache(None)(B.gnmr_clip_gradients_workspace)
 _ACTIVATIONS = {"silu": B.GNMR_ACT_SILU, "gelu": B.GNMR_ACT_GELU}
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
@@ -318,14 +319,10 @@ def gated_dgrad(dy, w, pre, offsets=None, mask=None, mask_value=1, activation="s
     return dpre
 
 
-def _rows_of(name, t, dtype, cols):
-    """t's rows over its last dimension, at any stride, as a matrix."""
-    if t.dtype != dtype or not t.is_cuda or t.dim() < 1:
-        raise TypeError(f"{name} must be a {dtype} tensor of rows on a HIP device")
-    if t.shape[-1] != cols:
-        raise ValueError(f"{name} must have {cols} columns, not {t.shape[-1]}")
-    flat = t if t.dim() == 2 else t.reshape(-1, cols)
-    rows = flat.shape[0]
+def _rows_of(t):
+    """t's rows over its last dimension, as a matrix whose rows the kernels can read where they lie."""
+    flat = t if t.dim() == 2 else t.reshape(-1, t.shape[-1])
+    rows, cols = flat.shape
     if (cols > 1 and flat.stride(1) != 1) or (rows > 1 and flat.stride(0) < cols):
         flat = flat.contiguous()
     return flat
@@ -335,42 +332,53 @@ def _row_stride(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _vector(name, t, cols, like, dtypes):
-    if t is not None and (t.dtype not in dtypes or t.shape != (cols,) or t.device != like.device or
-                          not t.is_contiguous()):
-        raise TypeError(f"{name} must be a contiguous tensor of {cols} values on x's device, of type "
-                        f"{' or '.join(str(d) for d in dtypes)}")
-    return t
+def _vectors(x, cols, **vectors):
+    """The type of the weight and bias of layer norm, those that there are."""
+    kind = None
+    for name, t in vectors.items():
+        if t is None:
+            continue
+        if t.dtype not in _DTYPES or t.shape != (cols,) or t.device != x.device or \
+                not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous bf16 or fp32 tensor of {cols} values on x's "
+                            "device")
+        if kind not in (None, t.dtype):
+            raise TypeError("weight and bias must be of one type")
+        kind = t.dtype
+    return kind or torch.float32
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
     """(y, mean, rstd): layer norm over x's last dimension, y = (x - mean) rstd weight + bias, and
     the fp32 statistics of each row that layer_norm_backward takes.  x: bf16 or fp32, any leading
     dimensions and row strides; weight and bias: bf16 or fp32, of one type, or None."""
-    if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 1:
+    kind = _DTYPES.get(x.dtype)
+    if kind is None or not x.is_cuda or x.dim() < 1:
         raise TypeError("x must be a bf16 or fp32 tensor of rows on a HIP device")
-    cols = x.shape[-1]
-    flat = _rows_of("x", x, x.dtype, cols)
-    _vector("weight", weight, cols, x, tuple(_DTYPES))
-    _vector("bias", bias, cols, x, tuple(_DTYPES) if weight is None else (weight.dtype,))
-    wt = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+    shape, where = x.shape, x.device
+    cols = shape[-1]
+    wt = _DTYPES[_vectors(x, cols, weight=weight, bias=bias)]
+    flat = _rows_of(x)
     if out is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x) if flat is x and x.is_contiguous() else torch.empty(
+            shape, dtype=x.dtype, device=where)
     else:
         y = out
-        if y.shape != x.shape or y.dtype != x.dtype or y.device != x.device or \
+        if y.shape != shape or y.dtype != x.dtype or y.device != where or \
                 (y.dim() != 2 and not y.is_contiguous()) or \
                 (y.dim() == 2 and ((cols > 1 and y.stride(1) != 1) or
                                    (y.shape[0] > 1 and y.stride(0) < cols))):
             raise TypeError("out must have x's shape, type and device, and contiguous rows")
     yflat = y if y.dim() == 2 else y.view(-1, cols)
     rows = flat.shape[0]
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    mean = torch.empty(rows, dtype=torch.float32, device=where)
+    if len(shape) != 2:
+        mean = mean.view(shape[:-1])
+    rstd = torch.empty_like(mean)
     device, stream = _on(x)
     with device:
-        B.gnmr_layer_norm(flat, _DTYPES[x.dtype], _row_stride(flat), weight, bias, _DTYPES[wt],
-                          yflat, _row_stride(yflat), mean, rstd, rows, cols, eps, stream)
+        B.gnmr_layer_norm(flat, kind, _row_stride(flat), weight, bias, wt, yflat,
+                          _row_stride(yflat), mean, rstd, rows, cols, eps, stream)
     return y, mean, rstd
 
 
@@ -379,30 +387,38 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, bias=False, input_grad=T
     """(dx, dweight, dbias) of layer_norm, from dy (of x's type and shape) and what it returned.
     dweight comes with a weight, in its type; dbias where bias is asked for, in that type too, or
     fp32 without a weight; input_grad and weight_grad False leave dx and dweight out (None)."""
-    if x.dtype not in _DTYPES or not x.is_cuda or x.dim() < 1:
+    kind = _DTYPES.get(x.dtype)
+    if kind is None or not x.is_cuda or x.dim() < 1:
         raise TypeError("x must be a bf16 or fp32 tensor of rows on a HIP device")
-    cols = x.shape[-1]
-    if dy.shape != x.shape:
-        raise ValueError(f"dy must have x's shape {tuple(x.shape)}")
-    xs, ds = _rows_of("x", x, x.dtype, cols), _rows_of("dy", dy, x.dtype, cols)
+    shape, where = x.shape, x.device
+    cols = shape[-1]
+    if dy.shape != shape:
+        raise ValueError(f"dy must have x's shape {tuple(shape)}")
+    if dy.dtype != x.dtype:
+        raise TypeError(f"dy must be of x's type, {x.dtype}")
     for name, t in (("mean", mean), ("rstd", rstd)):
-        if t.dtype != torch.float32 or t.shape != x.shape[:-1] or not t.is_contiguous():
+        if t.dtype != torch.float32 or t.shape != shape[:-1] or not t.is_contiguous():
             raise TypeError(f"{name} must be a contiguous fp32 tensor of an entry per row")
-    _vector("weight", weight, cols, x, tuple(_DTYPES))
+    type_ = _vectors(x, cols, weight=weight)
     _same_device(x, dy, mean, rstd)
-    wt = torch.float32 if weight is None else weight.dtype
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if input_grad else None
-    dw = torch.empty(cols, dtype=wt, device=x.device) if weight is not None and weight_grad else None
-    db = torch.empty(cols, dtype=wt, device=x.device) if bias else None
-    rows = xs.shape[0]
-    n = 0
+    xs, ds = _rows_of(x), _rows_of(dy)
+    dx = dw = db = work = None
+    if input_grad:
+        dx = torch.empty_like(x) if xs is x and x.is_contiguous() else torch.empty(
+            shape, dtype=x.dtype, device=where)
+    if weight is not None and weight_grad:
+        dw = torch.empty_like(weight)
+    if bias:
+        db = torch.empty(cols, dtype=type_, device=where)
+    rows, n = xs.shape[0], 0
     if dw is not None or db is not None:
         n = B.gnmr_layer_norm_backward_workspace(rows, cols)
-    work = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+        if n:
+            work = torch.empty(n, dtype=torch.uint8, device=where)
     device, stream = _on(x)
     with device:
-        B.gnmr_layer_norm_backward(ds, _row_stride(ds), xs, _DTYPES[x.dtype], _row_stride(xs), mean,
-                                   rstd, weight, _DTYPES[wt], dx, cols, dw, db, rows, cols, work, n,
+        B.gnmr_layer_norm_backward(ds, _row_stride(ds), xs, kind, _row_stride(xs), mean, rstd,
+                                   weight, _DTYPES[type_], dx, cols, dw, db, rows, cols, work, n,
                                    stream)
     return dx, dw, db
 
@@ -416,31 +432,38 @@ def clip_gradients(gradients, max_norm, out=None, known=(), norms=None, eps=1e-6
     in place are not touched."""
     gradients = list(gradients)
     outs = gradients if out is None else list(out)
+    count, known = len(gradients), set(known)
     if not gradients:
         raise ValueError("no gradient given")
-    if len(outs) != len(gradients):
-        raise ValueError(f"out must have {len(gradients)} tensors, not {len(outs)}")
-    known, like = set(known), gradients[0]
-    if not known.issubset(range(len(gradients))):
-        raise ValueError("known must be indexes of gradients")
-    if known and norms is None:
-        raise ValueError("known gradients need norms")
+    if len(outs) != count:
+        raise ValueError(f"out must have {count} tensors, not {len(outs)}")
+    like = gradients[0]
+    device = like.device
+    if known:
+        if not known.issubset(range(count)):
+            raise ValueError("known must be indexes of gradients")
+        if norms is None:
+            raise ValueError("known gradients need norms")
     if norms is not None and (norms.dtype != torch.float64 or not norms.is_contiguous() or
-                              norms.device != like.device):
+                              norms.device != device):
         raise TypeError("norms must be a contiguous float64 tensor on the gradients' device")
-    table, device = [], like.device
-    for k, (g, o) in enumerate(zip(gradients, outs)):
-        if g.dtype not in _DTYPES or not g.is_cuda or not g.is_contiguous():
-            raise TypeError(f"gradient {k} must be a contiguous bf16 or fp32 tensor on a HIP device")
-        if g.device != device:
+
+    def types(name, tensors):
+        kinds = [_DTYPES.get(t.dtype) for t in tensors]
+        if None in kinds or not all([t.is_contiguous() for t in tensors]) or not like.is_cuda:
+            raise TypeError(f"every {name} must be a contiguous bf16 or fp32 tensor on a HIP device")
+        if [t.device for t in tensors].count(device) != count:
             raise ValueError("all gradients must be on one device")
-        if o is not g and (o.dtype not in _DTYPES or o.device != device or o.shape != g.shape or
-                           not o.is_contiguous()):
-            raise TypeError(f"out {k} must be a contiguous bf16 or fp32 tensor of its gradient's shape "
-                            "and device")
-        table.append((g, o, g.numel(), _DTYPES[g.dtype], _DTYPES[o.dtype], k in known))
+        return kinds
+    kinds = out_kinds = types("gradient", gradients)
+    if out is not None:
+        out_kinds = types("out", outs)
+        if any([o.shape != g.shape for g, o in zip(gradients, outs)]):
+            raise ValueError("every out must have its gradient's shape")
+    table = list(zip(gradients, outs, [g.numel() for g in gradients], kinds, out_kinds,
+                     [k in known for k in range(count)] if known else [0] * count))
     norm = torch.empty((), dtype=torch.float64, device=device)
-    n = B.gnmr_clip_gradients_workspace(len(table))
+    n = _clip_workspace(count)
     work = torch.empty(n, dtype=torch.uint8, device=device)
     context, stream = _on(like)
     with context:

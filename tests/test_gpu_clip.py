@@ -260,7 +260,7 @@ def test_refusals():
                     (TypeError, lambda: t.clip_gradients([g.t()], 1.0)),
                     (TypeError, lambda: t.clip_gradients([g.cpu()], 1.0)),
                     (TypeError, lambda: t.clip_gradients([g], 1.0, out=[g.half()])),
-                    (TypeError, lambda: t.clip_gradients([g], 1.0, out=[g.flatten().clone()])),
+                    (ValueError, lambda: t.clip_gradients([g], 1.0, out=[g.flatten().clone()])),
                     (TypeError, lambda: t.clip_gradients([g], 1.0, norms=norms.float())),
                     (TypeError, lambda: t.clip_gradients([g], 1.0, norms=norms.cpu())),
                     (ValueError, lambda: t.clip_gradients([g], 1.0, known=[1], norms=norms)),
