@@ -205,18 +205,29 @@ double us_of_tiles(double tiles, double steps, double bytes) {
 // two, of which the quarters take 155 to 210 (us_of_tiles would say 97).
 constexpr int kSplitSteps = 32;
 
+// Microseconds that a tile's end takes for `beside` bytes beside each value of its result: in a 256
+// tile nothing covers them, in smaller ones the CU's other workgroup does in part.  d of 24,576 rows in
+// 64 groups, 2048 to 1408 (6 bytes): 289 us in 256 tiles, 237 in 128 tiles.
+template <int kT>
+double us_beside(double tiles, double beside) {
+  return tiles * kT * kT * beside / (kT == 256 ? 4.6e6 : 6.4e6);
+}
+
 // The tile edge of a product of grouped rows, N columns and `steps` K steps, whose weights have
-// `weight` bytes a value.  The groups' sizes are not known here: each is taken to leave half a
-// tile empty.
-inline int grouped_tile(const GroupArgs& g, int N, int K, int weight) {
+// `weight` bytes a value, and each value of the result `beside` more than its own two.  The groups'
+// sizes are not known here: each is taken to leave half a tile empty.
+inline int grouped_tile(const GroupArgs& g, int N, int K, int weight, double beside = 0.0) {
   const double rows = g.rows, steps = ceil(double(K) * weight / 128.0);
   const double used = std::min<double>(g.num, rows);  // groups with rows, at most
   const double empty = g.offsets == nullptr ? 0.0 : 0.5 * used;
   const double bytes = rows * (double(K) * weight + 2.0 * N) + used * N * double(K) * weight;
   auto tiles = [&](double t) { return ceil(rows / t + empty) * ceil(N / t); };
-  const double us64 = us_of_tiles<64>(tiles(64.0), steps, bytes);
-  const double us128 = us_of_tiles<128>(tiles(128.0), steps, bytes);
-  const double us256 = us_of_tiles<256>(tiles(256.0), steps, bytes);
+  const double us64 = us_of_tiles<64>(tiles(64.0), steps, bytes) +
+                      us_beside<64>(tiles(64.0), beside);
+  const double us128 = us_of_tiles<128>(tiles(128.0), steps, bytes) +
+                      us_beside<128>(tiles(128.0), beside);
+  const double us256 = us_of_tiles<256>(tiles(256.0), steps, bytes) +
+                       us_beside<256>(tiles(256.0), beside);
   return us64 <= us128 && us64 <= us256 ? 64 : us128 <= us256 ? 128 : 256;
 }
 
@@ -266,8 +277,8 @@ struct RowLaunch {
   int64_t most;   // tiles, at most
   bool split;     // of 256 tiles only those of whole rounds, and a launch of the rest in quarters
 };
-inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight) {
-  RowLaunch r{grouped_tile(g, N, K, weight), 0, 0, false};
+inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight, double beside = 0.0) {
+  RowLaunch r{grouped_tile(g, N, K, weight, beside), 0, 0, false};
   r.tiles_n = (N + r.tile - 1) / r.tile;
   r.most = most_row_tiles(g, r.tile) * r.tiles_n;
   if (r.tile < 256) return r;
@@ -277,20 +288,21 @@ inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight) {
   return r;
 }
 
-// The launches of a gated block's projections: of 2 H columns, in tiles of as many gate columns as
-// others; a 64 tile is 128 columns wide.
-inline RowLaunch gated_launch(const GroupArgs& g, int H, int K) {
-  RowLaunch r = row_launch(g, 2 * H, K, 2);
-  if (r.tile > 64) return r;
-  r.tiles_n = (H + 63) / 64;
-  r.most = most_row_tiles(g, 64) * r.tiles_n;
-  return r;
-}
+// Bytes that a value of the gated gradient's product costs beside its own: two of p are read, and two written.
+constexpr double kGatedDgradBeside = 6.0;
+
+// Whether a gated block's 64 tiles, which then mostly have a group's rows in one, read its weights
+// past the caches.  us through and past the
+// caches: 64 experts 2048 x 1408, 48 rows 85 and 77.5, 1,536 rows 146 and 133; 8 of 4096 x 11008, 64
+// rows 249 and 223 (6.5 TB/s).
+inline bool gated_weights_once(const GroupArgs& g) { return g.rows <= 64 * int64_t(g.num); }
 
 // Makes them: launch(edge, share, workgroups), with *tiles_n set.
 template <class Launch>
-void launch_tiles(const RowLaunch& r, int32_t* tiles_n, Launch&& launch) {
+void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* tiles_n,
+                      Launch&& launch, double beside = 0.0) {
   using std::integral_constant;
+  const RowLaunch r = row_launch(g, N, K, weight, beside);
   *tiles_n = r.tiles_n;
   const integral_constant<Share, kAll> all;
   if (r.tile == 64) return launch(integral_constant<int, 64>{}, all, r.most);
@@ -299,11 +311,6 @@ void launch_tiles(const RowLaunch& r, int32_t* tiles_n, Launch&& launch) {
   launch(integral_constant<int, 256>{}, integral_constant<Share, kRounds>{}, r.most);
   launch(integral_constant<int, 128>{}, integral_constant<Share, kRest>{},
          std::min<int64_t>(4 * r.most, 512));
-}
-template <class Launch>
-void launch_row_tiles(const GroupArgs& g, int N, int K, int weight, int32_t* tiles_n,
-                      Launch&& launch) {
-  launch_tiles(row_launch(g, N, K, weight), tiles_n, launch);
 }
 
 // Tile *v of group *e for workgroup w, of `num` groups with `per` tiles each.  Where a group has

@@ -69,20 +69,20 @@ __device__ __forceinline__ Act act(float g) {
   }
 }
 
-// Tiles of kT rows and kTN columns, kTN / 2 of gate and as many of the up projection.  (A
-// wavefront needs 64 columns for a block of each: a 64 tile is 128 wide.)
-template <int kT>
+// Tiles of kT rows and kT columns, kT / 2 of gate and as many of the up projection.  kOnce: the
+// weights are read past the caches.
+template <int kT, bool kOnce>
 struct GatedTile {
-  static constexpr int kTN = kT == 64 ? 128 : kT, kHidden = kTN / 2;
-  static constexpr int kStep = 128, kStages = kT == 64 ? 3 : 2, kPerCu = kT == 256 ? 1 : 2;
-  using T = mm::Tile<Bf16, false, false, kT, kTN, 2, kStep, kStages, false,
-                     mm::PairedOperand<Bf16, kTN, kStep>>;
+  static constexpr int kHidden = kT / 2;
+  using D = mm::Depth<false, false, kT>;
+  using T = mm::Tile<Bf16, false, false, kT, kT, 2, D::kStep, D::kStages, false,
+                     mm::PairedOperand<Bf16, kT, D::kStep, kOnce>>;
 };
 
-template <int kAct, bool kKeep, int kT, Share kShare>
-__global__ __launch_bounds__(mm::kThreads, (GatedTile<kT>::kPerCu)) void k9_linear(
+template <int kAct, bool kKeep, int kT, Share kShare, bool kOnce>
+__global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, false, kT>::kPerCu)) void k9_linear(
     const GatedLinear a) {
-  using G = GatedTile<kT>;
+  using G = GatedTile<kT, kOnce>;
   using T = typename G::T;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   RowTile t;
@@ -104,10 +104,10 @@ __global__ __launch_bounds__(mm::kThreads, (GatedTile<kT>::kPerCu)) void k9_line
           return u32x2{pack(a0, a1), pack(a2, a3)};
         },
         [&](int m, int n, const u32x4& v) {
-          const int j = h0 + (n >> 6) * 32 + (n & 31);
+          const int j = h0 + (n >> 5) * 16 + (n & 15);
           if (m < t.rows && j < a.H)
             put(reinterpret_cast<u32x4*>(a.pre + int64_t(t.row + m) * a.pre_stride +
-                                         (n & 32 ? a.H : 0) + j), v, a.past);
+                                         (n & 16 ? a.H : 0) + j), v, a.past);
         });
   }
   T::out16_joined(
@@ -207,10 +207,16 @@ template <int kAct, bool kKeep>
 void launch_linear_of(GatedLinear a, hipStream_t s) {
   a.past = past_caches(a.g.rows, int64_t(a.H) * (kKeep ? 3 : 1));
   auto launch = [&](auto edge, auto share, int64_t wgs) {
-    hipLaunchKernelGGL((k9_linear<kAct, kKeep, decltype(edge)::value, decltype(share)::value>),
-                       dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
+    constexpr int kT = decltype(edge)::value;
+    auto of = [&](auto once) {
+      hipLaunchKernelGGL((k9_linear<kAct, kKeep, kT, decltype(share)::value,
+                                    kT == 64 && decltype(once)::value>),
+                         dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
+    };
+    if (kT == 64 && gated_weights_once(a.g)) of(std::true_type{});
+    else of(std::false_type{});
   };
-  launch_tiles(gated_launch(a.g, a.H, a.K), &a.tiles_n, launch);
+  launch_row_tiles(a.g, 2 * a.H, a.K, 2, &a.tiles_n, launch);
 }
 
 template <int kAct>
@@ -220,7 +226,7 @@ void launch_dgrad_of(GatedDgrad a, hipStream_t s) {
     hipLaunchKernelGGL((k9_dgrad<kAct, decltype(edge)::value, decltype(share)::value>),
                        dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);
   };
-  launch_row_tiles(a.g, a.H, a.K, 2, &a.tiles_n, launch);
+  launch_row_tiles(a.g, a.H, a.K, 2, &a.tiles_n, launch, kGatedDgradBeside);
 }
 
 }  // namespace

@@ -80,8 +80,8 @@ __device__ __forceinline__ void lanes_meet() {
 }
 
 // One operand of a tile: kT rows (m or n) of which `rows` exist.  kStep: bytes of a K
-// step in a "rows" operand.
-template <class E, bool kCols, int kT, int kStep>
+// step in a "rows" operand.  kOnce: what it reads is not read again by other tiles.
+template <class E, bool kCols, int kT, int kStep, bool kOnce = false>
 struct Operand {
   static_assert(!kCols || E::kBytes == 2, "k as the slow index: 16-bit types only");
   static_assert(!kCols || kT >= 64, "the swizzle of a cols operand takes four units a row");
@@ -139,7 +139,7 @@ struct Operand {
     for (int q = lo; q < hi; ++q)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           r, (__attribute__((address_space(3))) void*)(lds + (wave * kLoads + q) * 1024), 16,
-          off[q], 0, 0, 0);
+          off[q], 0, 0, kOnce ? 2 : 0);  // 2: past the caches
   }
 
   // Parts [lo, hi) of step s, of which only `left` values of k exist, the others zero.
@@ -171,19 +171,19 @@ struct Operand {
   }
 };
 
-// A "rows" operand of kT / 2 rows of each of two matrices of one shape, in blocks of 32 by turns:
-// tile row 64 p + r is row 32 p + r of the first for r < 32, row 32 p + r - 32 of the second above.
-// What belongs together is then in the same registers of two neighbouring accumulators.
-template <class E, int kT, int kStep>
+// A "rows" operand of kT / 2 rows of each of two matrices of one shape, in runs of 16 by turns: tile
+// row 32 p + r is row 16 p + r of the first for r < 16, row 16 p + r - 16 of the second above.  What
+// belongs together is then in the same lane: in register groups g and g + 2 of an accumulator.
+template <class E, int kT, int kStep, bool kOnce = false>
 struct PairedOperand {
-  typedef Operand<E, false, kT, kStep> Op;
+  typedef Operand<E, false, kT, kStep, kOnce> Op;
   static constexpr int kBytes = Op::kBytes, kLoads = Op::kLoads;
-  static_assert(Op::kPer <= 32, "an instruction's rows are of one matrix");
+  static_assert(Op::kPer <= 16, "an instruction's rows are of one matrix");
   Op op;
   int64_t apart;   // bytes from the first matrix to the second
 
   static __device__ __forceinline__ int second(int q, int wave) {
-    return ((wave * Op::kLoads + q) * Op::kPer >> 5) & 1;
+    return ((wave * Op::kLoads + q) * Op::kPer >> 4) & 1;
   }
 
   // `rows` of the rows exist in each matrix.
@@ -196,7 +196,7 @@ struct PairedOperand {
 #pragma unroll
     for (int q = 0; q < Op::kLoads; ++q) {
       const int row = (wave * Op::kLoads + q) * Op::kPer + lane / Op::kChunks;
-      const int of = (row >> 6) * 32 + (row & 31), slot = lane % Op::kChunks;
+      const int of = (row >> 5) * 16 + (row & 15), slot = lane % Op::kChunks;
       op.off[q] = uint32_t(of < rows ? of : rows - 1) * op.ld + 16u * (slot ^ Op::spread(row));
     }
   }
@@ -496,7 +496,7 @@ struct Tile {
   template <class Join, class Put>
   static __device__ __forceinline__ void out16_joined(const Acc (&acc)[kBM][kBN], int wave, int lane,
                                                       Join&& join, Put&& put) {
-    static_assert(!kSwap && kBN % 2 == 0, "pairs of column blocks");
+    static_assert(!kSwap, "the groups of four are columns");
     constexpr int kRowBytes = kCols, kChunks = kRowBytes / 16, kAtOnce = 64 / kChunks;
     constexpr int kPass = pass(kRowBytes);
     static_assert(kRows / 32 % kPass == 0 && kPass * 32 * kRowBytes <= kRegion, "whole passes");
@@ -506,15 +506,16 @@ struct Tile {
 #pragma unroll
     for (int p = 0; p < kRows / 32; p += kPass) {
 #pragma unroll
-      for (int j = 0; j < kCols / 64; ++j)
+      for (int j = 0; j < kCols / 32; ++j)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
           for (int i = 0; i < kPass; ++i) {
-            const int row = 32 * i + (lane & 31), col = 32 * j + 8 * g + 4 * (lane >> 5);
-            const Acc &a = acc[p + i][2 * j], &b = acc[p + i][2 * j + 1];
-            const u32x2 v = join(f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]},
-                                 f32x4{b[4 * g], b[4 * g + 1], b[4 * g + 2], b[4 * g + 3]});
+            const int row = 32 * i + (lane & 31), col = 16 * j + 8 * g + 4 * (lane >> 5);
+            const Acc& a = acc[p + i][j];
+            const u32x2 v =
+                join(f32x4{a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]},
+                     f32x4{a[4 * g + 8], a[4 * g + 9], a[4 * g + 10], a[4 * g + 11]});
             *reinterpret_cast<u32x2*>(chunk<kRowBytes>(at, row, col / 8) + 8 * (lane >> 5)) = v;
           }
       lanes_meet();

@@ -17,9 +17,12 @@ int main() {
   while (scanf("%15s %d %d %d %d", op, &rows, &groups, &hidden, &others) == 5) {
     const gnmr::GroupArgs g{groups == 0 ? nullptr : &kOffsets, nullptr, groups == 0 ? 1 : groups, 1,
                             rows};
-    const gnmr::RowLaunch r = !strcmp(op, "linear") ? gnmr::gated_launch(g, hidden, others)
-                                                    : gnmr::row_launch(g, hidden, others, 2);
-    printf("%d %s\\n", r.tile, r.split ? "rounds and rest" : "all");
+    const gnmr::RowLaunch r = !strcmp(op, "linear") ? gnmr::row_launch(g, 2 * hidden, others, 2)
+                                                    : gnmr::row_launch(
+                                                          g, hidden, others, 2,
+                                                          gnmr::kGatedDgradBeside);
+    printf("%d %s%s\\n", r.tile, r.split ? "rounds and rest" : "all",
+           !strcmp(op, "linear") && r.tile == 64 && gnmr::gated_weights_once(g) ? " once" : "");
   }
 }
 """
@@ -48,7 +51,7 @@ def build(folder):
 # nobody, and what the projections and their gradient run in; the features are no multiples of a
 # step's 64 values
 SHAPES = {
-    "64 tiles, 70 experts": (88, 72, loads(70, 600, 1), 5, ("64 all", "64 all")),
+    "64 tiles, 70 experts": (88, 72, loads(70, 600, 1), 5, ("64 all once", "64 all")),
     "64 tiles, one expert": (80, 136, None, 333, ("64 all", "64 all")),
     "128 tiles, 70 experts": (488, 200, loads(70, 300, 2), 9, ("128 all", "64 all")),
     "128 tiles, 8 experts": (856, 360, loads(8, 1200, 4), 70, ("128 all", "64 all")),
@@ -56,8 +59,8 @@ SHAPES = {
     "256 tiles, 100 experts": (608, 136, loads(100, 200, 5), 3, ("256 all", "128 all")),
     "256 tiles, 8 experts": (2880, 136, loads(8, 920, 6), 33, ("256 all", "128 all")),
     "256 tiles, one expert": (200, 136, None, 18500, ("256 all", "128 all")),
-    "256 tiles of the gradient": (2880, 136, loads(8, 2400, 7), 33, ("128 all", "256 all")),
-    "256 tiles of the gradient, one expert": (392, 136, None, 18500, ("128 all", "256 all")),
+    "256 tiles of the gradient": (2000, 1000, loads(8, 4000, 7), 33, ("128 all", "256 all")),
+    "256 tiles of the gradient, one expert": (2000, 520, None, 5000, ("128 all", "256 all")),
     "rounds and rest, 8 experts": (2504, 5128, loads(8, 4200, 8), 259,
                                    ("256 rounds and rest", "256 rounds and rest")),
     "rounds and rest of the gradient, one expert": (3816, 5128, None, 10115,
