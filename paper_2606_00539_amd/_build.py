@@ -16,8 +16,8 @@ SOURCES = [os.path.join(PKG, "csrc", f)
                      "k9_gated.hip", "k10_layer_norm.hip", "k11_clip.hip")]
 HEADERS = [os.path.join(PKG, "csrc", f)
            for f in ("gnmr_internal.h", "groups.h", "host_call.h", "k1_geometry.h", "k1_item.h",
-                     "k3_pool.h", "k8_range.h", "lane_ops.h", "launch_tag.h", "mm_tile.h", "row_checks.h",
-                     "unit_step.h", "values.h")] + [os.path.join(ROOT, "include", "gnmr.h")]
+                     "k3_pool.h", "k8_range.h", "lane_ops.h", "launch_tag.h", "mm_stream.h", "mm_tile.h",
+                     "row_checks.h", "unit_step.h", "values.h")] + [os.path.join(ROOT, "include", "gnmr.h")]
 
 # Marshalling of the per-step calls (host code), for the Python that builds it: the
 # name carries that Python's ABI, so that no other one loads it.

@@ -216,7 +216,8 @@ double us_beside(double tiles, double beside) {
 // The tile edge of a product of grouped rows, N columns and `steps` K steps, whose weights have
 // `weight` bytes a value, and each value of the result `beside` more than its own two.  The groups'
 // sizes are not known here: each is taken to leave half a tile empty.
-inline int grouped_tile(const GroupArgs& g, int N, int K, int weight, double beside = 0.0) {
+inline int grouped_tile(const GroupArgs& g, int N, int K, int weight, double beside = 0.0,
+                        double* us = nullptr) {
   const double rows = g.rows, steps = ceil(double(K) * weight / 128.0);
   const double used = std::min<double>(g.num, rows);  // groups with rows, at most
   const double empty = g.offsets == nullptr ? 0.0 : 0.5 * used;
@@ -228,7 +229,25 @@ inline int grouped_tile(const GroupArgs& g, int N, int K, int weight, double bes
                       us_beside<128>(tiles(128.0), beside);
   const double us256 = us_of_tiles<256>(tiles(256.0), steps, bytes) +
                        us_beside<256>(tiles(256.0), beside);
+  if (us != nullptr) *us = std::min(us64, std::min(us128, us256));
   return us64 <= us128 && us64 <= us256 ? 64 : us128 <= us256 ? 128 : 256;
+}
+
+// Tiles of products one after the other on a CU (mm_stream.h), and whether that is the way for a
+// product of grouped rows, `bytes` of memory to each value of whose result are read and written at its
+// tiles' ends.  A step takes 0.70 us, the end of a tile 7 and its bytes 32 KB to a us; us that
+// were measured, and in tiles of the best edge: 24,576 rows in 64 groups, 2048 to 2 x 1408 (3 bytes)
+// 360 and 402, the gradient (8 bytes) 226 and 239; 8,192 rows, 4096 to 2 x 11008 1,195 and 1,150.
+constexpr int kStreamM = 128, kStreamN = 256;
+inline bool streams(const GroupArgs& g, int N, int K, double beside, double bytes) {
+  if (K % 64 != 0 || K < 256) return false;     // (whole steps, two rounds of three at least)
+  double tiles_us;
+  grouped_tile(g, N, K, 2, beside, &tiles_us);
+  const double used = std::min<double>(g.num, g.rows);
+  const double tiles = ceil(double(g.rows) / kStreamM + (g.offsets == nullptr ? 0.0 : 0.5 * used)) *
+                       ceil(double(N) / kStreamN);
+  const double steps = ceil(K / 192.0) * 3.0;
+  return ceil(tiles / 256.0) * (0.70 * steps + 7.0 + kStreamM * kStreamN * bytes / 32e3) < tiles_us;
 }
 
 // The launches of a batch of products of K8: X X^T and A A, symmetric (tiles on and above the
@@ -290,6 +309,12 @@ inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight, double
 
 // Bytes that a value of the gated gradient's product costs beside its own: two of p are read, and two written.
 constexpr double kGatedDgradBeside = 6.0;
+inline bool gated_linear_streams(const GroupArgs& g, int H, int K, bool keep) {
+  return streams(g, 2 * H, K, keep ? 1.0 : 0.0, keep ? 3.0 : 1.0);
+}
+inline bool gated_dgrad_streams(const GroupArgs& g, int H, int K) {
+  return streams(g, H, K, kGatedDgradBeside, kGatedDgradBeside + 2.0);
+}
 
 // Whether a gated block's 64 tiles, which then mostly have a group's rows in one, read its weights
 // past the caches.  us through and past the

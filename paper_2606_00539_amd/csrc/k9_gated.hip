@@ -16,6 +16,7 @@
 #include "gnmr_internal.h"
 #include "groups.h"
 #include "lane_ops.h"
+#include "mm_stream.h"
 #include "mm_tile.h"
 
 namespace gnmr {
@@ -124,6 +125,165 @@ __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, false, kT>::kPerCu)
       });
 }
 
+// 16-byte chunk c of row r of a part of rows of kRowBytes staged in LDS: rows start in other banks.
+template <int kRowBytes>
+__device__ __forceinline__ char* chunk(char* at, int r, int c) {
+  return at + r * kRowBytes + 16 * (c ^ (r & (kRowBytes / 16 - 1)));
+}
+
+// The same with the tiles of a compute unit one after the other (mm_stream.h); K a multiple of 64.
+template <int kAct, bool kKeep, bool kPast>
+__global__ __launch_bounds__(mm::kThreads, 1) void k9_linear_stream(const GatedLinear a) {
+  using T = mm::Tile<Bf16, false, false, kStreamM, kStreamN, 2, 128, 3, false,
+                     mm::PairedOperand<Bf16, kStreamN, 128>>;
+  constexpr int kHidden = kStreamN / 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t half = int64_t(a.H) * a.K;
+  auto place = [&](const RowTile& t, typename T::OpM* om, typename T::OpN* on) {
+    const int h0 = t.tn * kHidden;
+    const bool owned = t.group < a.g.num;
+    om->at(a.x + int64_t(t.row) * a.x_stride, a.x_stride * 2, t.rows, wave, lane);
+    on->at(a.w + (owned ? t.group * 2 * half : 0) + int64_t(h0) * a.K, half * 2, int64_t(a.K) * 2,
+           a.H - h0, wave, lane);
+    return owned;
+  };
+  const int m0 = T::first_row(wave), n0 = T::first_col(wave);
+  auto out = [&](const typename T::Acc(&acc)[T::kBM][T::kBN], const RowTile& t, char* lds) {
+    const int h0 = t.tn * kHidden;
+    auto four = [&](int i, int j, int g) {
+      const typename T::Acc& v = acc[i][j];
+      return f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+    };
+#pragma unroll
+    for (int i = 0; i < T::kBM; ++i) {
+      const int row = lane & 31;
+      if constexpr (kKeep) {
+#pragma unroll
+        for (int j = 0; j < T::kBN; ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<u32x2*>(chunk<256>(lds, row, 4 * j + g) + 8 * (lane >> 5)) =
+                pack(four(i, j, g));
+        mm::lanes_meet();
+        char* const to = reinterpret_cast<char*>(a.pre + int64_t(t.row) * a.pre_stride + h0);
+#pragma unroll
+        for (int r = 0; r < 32; r += 4) {
+          const int m = m0 + 32 * i + r + lane / 16, n = n0 + 8 * (lane & 15);
+          const int col = (n >> 5) * 16 + (n & 15);
+          mm::store_if<kPast>(to, m < t.rows && h0 + col < a.H,
+                              2 * (uint32_t(m) * uint32_t(a.pre_stride) + (n & 16 ? a.H : 0) + col),
+                              *reinterpret_cast<const u32x4*>(chunk<256>(lds, r + lane / 16, lane & 15)));
+        }
+        mm::lanes_meet();
+      }
+#pragma unroll
+      for (int j = 0; j < T::kBN; ++j)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const f32x4 gate = four(i, j, g), up = four(i, j, g + 2);
+          f32x4 h;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = act<kAct>(gate[k]).value * up[k];
+          *reinterpret_cast<u32x2*>(chunk<128>(lds, row, 2 * j + g) + 8 * (lane >> 5)) = pack(h);
+        }
+      mm::lanes_meet();
+      char* const to = reinterpret_cast<char*>(a.h + int64_t(t.row) * a.h_stride + h0);
+#pragma unroll
+      for (int r = 0; r < 32; r += 8) {
+        const int m = m0 + 32 * i + r + lane / 8, col = n0 / 2 + 8 * (lane & 7);
+        mm::store_if<kPast>(to, m < t.rows && h0 + col < a.H,
+                            2 * (uint32_t(m) * uint32_t(a.h_stride) + col),
+                            *reinterpret_cast<const u32x4*>(chunk<128>(lds, r + lane / 8, lane & 7)));
+      }
+      mm::lanes_meet();
+    }
+  };
+  mm::stream<T, T::kBM * (kKeep ? 12 : 4)>(a.g, a.tiles_n, a.K, wave, lane, place, [](const RowTile&) {}, out);
+}
+
+template <int kAct, bool kPast>
+__global__ __launch_bounds__(mm::kThreads, 1) void k9_dgrad_stream(const GatedDgrad a) {
+  using T = mm::Tile<Bf16, false, true, kStreamM, kStreamN, 2, 128, 3>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto place = [&](const RowTile& t, typename T::OpM* om, typename T::OpN* on) {
+    const int n0 = t.tn * kStreamN;
+    const bool owned = t.group < a.g.num;
+    om->at(a.dy + int64_t(t.row) * a.dy_stride, a.dy_stride * 2, t.rows, wave, lane);
+    on->at(a.w + (owned ? int64_t(t.group) * a.H * a.K : 0) + n0, int64_t(a.H) * 2, a.H - n0, wave,
+           lane);
+    return owned;
+  };
+  // The wavefront's part of d goes out in parts of 32 x 64; a lane has eight columns of four rows of
+  // a part, whose p is on its way while the part before goes out.
+  constexpr int kParts = 2 * T::kBM, kPieces = 4;
+  u32x4 gate[2][kPieces], up[2][kPieces];
+  auto row = [&](int part, int q) {
+    return T::first_row(wave) + 32 * (part >> 1) + 8 * q + lane / 8;
+  };
+  auto col = [&](int part) { return T::first_col(wave) + 64 * (part & 1) + 8 * (lane & 7); };
+  auto fetch = [&](const RowTile& t, int part) {
+    // (rows and columns past the last ones read those)
+    const int n = min(t.tn * kStreamN + col(part), a.H - 8);
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+      const uint16_t* p =
+          a.pre + int64_t(t.row + min(row(part, q), t.rows - 1)) * a.pre_stride + n;
+      gate[part & 1][q] = *reinterpret_cast<const u32x4*>(p);
+      up[part & 1][q] = *reinterpret_cast<const u32x4*>(p + a.H);
+    }
+  };
+  auto out = [&](const typename T::Acc(&acc)[T::kBM][T::kBN], const RowTile& t, char* lds) {
+    // rows of nobody get 0, whatever their p holds
+    const uint32_t kept = t.group < a.g.num ? 0xFFFFFFFFu : 0u;
+    const int n0 = t.tn * kStreamN;
+    char* const to = reinterpret_cast<char*>(a.dpre + int64_t(t.row) * a.dpre_stride + n0);
+#pragma unroll
+    for (int part = 0; part < kParts; ++part) {
+      if (part + 1 < kParts) fetch(t, part + 1);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const typename T::Acc& v = acc[part >> 1][2 * (part & 1) + j];
+          *reinterpret_cast<f32x4*>(chunk<256>(lds, lane & 31, 8 * j + 2 * g + (lane >> 5))) =
+              f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+        }
+      mm::lanes_meet();
+#pragma unroll
+      for (int q = 0; q < kPieces; ++q) {
+        const u32x4 pg = gate[part & 1][q], pu = up[part & 1][q];
+        u32x4 dg, du;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const f32x4 d = *reinterpret_cast<const f32x4*>(
+              chunk<256>(lds, 8 * q + lane / 8, 2 * (lane & 7) + k));
+          const f32x4 g = four(u32x2{pg[2 * k], pg[2 * k + 1]}), u = four(u32x2{pu[2 * k], pu[2 * k + 1]});
+          f32x4 vg, vu;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const Act f = act<kAct>(g[e]);
+            vg[e] = d[e] * f.slope * u[e];
+            vu[e] = d[e] * f.value;
+          }
+          const u32x2 of_gate = pack(vg) & kept, of_up = pack(vu) & kept;
+          dg[2 * k] = of_gate.x;
+          dg[2 * k + 1] = of_gate.y;
+          du[2 * k] = of_up.x;
+          du[2 * k + 1] = of_up.y;
+        }
+        const int m = row(part, q), n = col(part);
+        const bool there = m < t.rows && n0 + n < a.H;
+        const uint32_t offset = 2 * (uint32_t(m) * uint32_t(a.dpre_stride) + n);
+        mm::store_if<kPast>(to, there, offset, dg);
+        mm::store_if<kPast>(to, there, offset + 2 * uint32_t(a.H), du);
+      }
+      mm::lanes_meet();
+    }
+  };
+  mm::stream<T, 2 * kParts * kPieces>(a.g, a.tiles_n, a.K, wave, lane, place,
+                                      [&](const RowTile& t) { fetch(t, 0); }, out);
+}
+
 template <int kAct, int kT, Share kShare>
 __global__ __launch_bounds__(mm::kThreads, (mm::Depth<false, true, kT>::kPerCu)) void k9_dgrad(
     const GatedDgrad a) {
@@ -206,6 +366,13 @@ __global__ __launch_bounds__(256) void k9_activation(const GatedActivation a) {
 template <int kAct, bool kKeep>
 void launch_linear_of(GatedLinear a, hipStream_t s) {
   a.past = past_caches(a.g.rows, int64_t(a.H) * (kKeep ? 3 : 1));
+  if (gated_linear_streams(a.g, a.H, a.K, kKeep)) {
+    a.tiles_n = (2 * a.H + kStreamN - 1) / kStreamN;
+    const dim3 grid(mm::kStreamWorkgroups), block(mm::kThreads);
+    if (a.past) hipLaunchKernelGGL((k9_linear_stream<kAct, kKeep, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k9_linear_stream<kAct, kKeep, false>), grid, block, 0, s, a);
+    return;
+  }
   auto launch = [&](auto edge, auto share, int64_t wgs) {
     constexpr int kT = decltype(edge)::value;
     auto of = [&](auto once) {
@@ -222,6 +389,13 @@ void launch_linear_of(GatedLinear a, hipStream_t s) {
 template <int kAct>
 void launch_dgrad_of(GatedDgrad a, hipStream_t s) {
   a.past = past_caches(a.g.rows, 2 * int64_t(a.H));
+  if (gated_dgrad_streams(a.g, a.H, a.K)) {
+    a.tiles_n = (a.H + kStreamN - 1) / kStreamN;
+    const dim3 grid(mm::kStreamWorkgroups), block(mm::kThreads);
+    if (a.past) hipLaunchKernelGGL((k9_dgrad_stream<kAct, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k9_dgrad_stream<kAct, false>), grid, block, 0, s, a);
+    return;
+  }
   auto launch = [&](auto edge, auto share, int64_t wgs) {
     hipLaunchKernelGGL((k9_dgrad<kAct, decltype(edge)::value, decltype(share)::value>),
                        dim3(unsigned(wgs)), dim3(mm::kThreads), 0, s, a);

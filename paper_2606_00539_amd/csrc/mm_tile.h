@@ -268,9 +268,10 @@ struct Depth {
 // kTM x kTN tiles by kWM x (4 / kWM) wavefronts.  kSwap: accumulator registers hold
 // four rows of a column instead of four columns of a row.  N: the N operand, where it is not an
 // Operand (PairedOperand).
-template <class E, bool kColsM, bool kColsN, int kTM, int kTN, int kWM, int kStep, int kStages,
+template <class E, bool kColsM, bool kColsN, int kTM, int kTN, int kWM, int kStep, int kStageCount,
           bool kSwap = false, class N = Operand<E, kColsN, kTN, kStep>>
 struct Tile {
+  static constexpr int kStages = kStageCount;
   static constexpr int kWN = kWaves / kWM;
   static constexpr int kWaveM = kTM / kWM, kWaveN = kTN / kWN;  // a wavefront's part
   static constexpr int kBM = kWaveM / 32, kBN = kWaveN / 32;
@@ -279,12 +280,19 @@ struct Tile {
   static constexpr int kStepK = OpM::kStepK;
   static constexpr int kStage = OpM::kBytes + OpN::kBytes;
   typedef typename E::Acc Acc;
+  typedef typename E::Frag Frag;
+  typedef Reader<E, kColsM, kTM, kStep, kBM> ReadM;
+  typedef Reader<E, kColsN, kTN, kStep, kBN> ReadN;
+  static __device__ __forceinline__ Acc mfma(Frag a, Frag b, Acc c) { return E::mfma(a, b, c); }
   static constexpr int kSlots = kStep / 32;  // matrix-core instructions deep
   static constexpr int kLoads = OpM::kLoads + OpN::kLoads;
   // Requests made in a step's last slot and up to the end of the next one's first.
   static constexpr int kFirst = kSlots == 2 ? kLoads : kLoads * 6 / 16;
   static constexpr int kSecond = kSlots == 2 ? kLoads : kLoads * 12 / 16;
   static_assert(kStages >= 2 && kStages <= 5, "stages");
+  // LDS reads of a slot, and how many are made beside each of its first products
+  static constexpr int kReads = kBM * (kColsM ? 2 : 1) + kBN * (kColsN ? 2 : 1);
+  static constexpr int kReadsEach = (kReads + (kBM * kBN + 1) / 2 - 1) / ((kBM * kBN + 1) / 2);
 
   // Stage k's memory.  (Distinct variables: the compiler then knows which requests a
   // read has to wait for.)
@@ -359,8 +367,7 @@ struct Tile {
     // fragments first, then, in a step's last slot, the requests, spread over the
     // matrix-core instructions.
     constexpr int kMfma = kBM * kBN;
-    constexpr int kReads = kBM * (kColsM ? 2 : 1) + kBN * (kColsN ? 2 : 1);
-    constexpr int kEach = (kReads + (kMfma + 1) / 2 - 1) / ((kMfma + 1) / 2);
+    constexpr int kEach = kReadsEach;
     auto order = [](auto loads) {
       constexpr int kL = decltype(loads)::value, kPer = (kL + kMfma - 1) / kMfma;
 #pragma unroll

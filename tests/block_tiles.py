@@ -17,6 +17,11 @@ int main() {
   while (scanf("%15s %d %d %d %d", op, &rows, &groups, &hidden, &others) == 5) {
     const gnmr::GroupArgs g{groups == 0 ? nullptr : &kOffsets, nullptr, groups == 0 ? 1 : groups, 1,
                             rows};
+    if (!strcmp(op, "linear") ? gnmr::gated_linear_streams(g, hidden, others, true)
+                              : gnmr::gated_dgrad_streams(g, hidden, others)) {
+      puts("stream");
+      continue;
+    }
     const gnmr::RowLaunch r = !strcmp(op, "linear") ? gnmr::row_launch(g, 2 * hidden, others, 2)
                                                     : gnmr::row_launch(
                                                           g, hidden, others, 2,
@@ -48,8 +53,8 @@ def build(folder):
 
 
 # hidden and the other features, the rows of the experts (None: one without offsets), rows of
-# nobody, and what the projections and their gradient run in; the features are no multiples of a
-# step's 64 values
+# nobody, and what the projections (kept) and their gradient run in; but for the streams' the other
+# features are no multiples of a step's 64 values
 SHAPES = {
     "64 tiles, 70 experts": (88, 72, loads(70, 600, 1), 5, ("64 all once", "64 all")),
     "64 tiles, one expert": (80, 136, None, 333, ("64 all", "64 all")),
@@ -65,6 +70,11 @@ SHAPES = {
                                    ("256 rounds and rest", "256 rounds and rest")),
     "rounds and rest of the gradient, one expert": (3816, 5128, None, 10115,
                                                     ("256 all", "256 rounds and rest")),
+    "streams, 70 experts": (1000, 2048, loads(70, 9000, 9), 300, ("stream", "stream")),
+    "streams, 4 experts": (5504, 4096, loads(4, 1000, 10), 5, ("stream", "stream")),
+    "stream of the gradient, one expert": (4096, 4096, None, 4093, ("256 all", "stream")),
+    "stream, one expert": (5504, 2048, None, 2041, ("stream", "256 all")),
+    "stream of the gradient, fewer than 256 tiles": (2752, 4096, None, 2000, ("256 all", "stream")),
     "rounds and rest, one expert": (1912, 5128, None, 10115, ("256 rounds and rest", "128 all")),
 }
 

@@ -10,5 +10,5 @@ def test_the_shapes_run_where_they_are_meant_to(tmp_path):
     assert [(n, g) for n, g, w in zip(names, got, want) if g != w] == []
     for w in ("linear", "dgrad"):
         assert {g for (v, _), g in zip(names, got) if v == w} == {
-            "64 all", "128 all", "256 all", "256 rounds and rest"} | (
+            "64 all", "128 all", "256 all", "256 rounds and rest", "stream"} | (
                 {"64 all once"} if w == "linear" else set())

@@ -215,9 +215,11 @@ def test_every_kernel(name):
         m[off[-1]:] = float("nan")
     kind = "gelu" if "one expert" in name else "silu"
     h, kept = t.gated_linear(x, w, d_off, activation=kind, keep=True)
+    say("  nothing kept")
+    alone = t.gated_linear(x, w, d_off, activation=kind)
     say("  gradient")
     dp = t.gated_dgrad(dy, v, pre, d_off, activation=kind)
-    assert not h[off[-1]:].any() and not kept[off[-1]:].any() and not dp[off[-1]:].any()
+    assert not any(m[off[-1]:].any() for m in (h, alone, kept, dp))
     rng = np.random.default_rng(6)
     # the first and the last row of some experts, and others
     pick = sorted({int(r) for e in rng.permutation(E)[:12] if off[e + 1] > off[e]
@@ -230,6 +232,7 @@ def test_every_kernel(name):
         got = host(kept[r:r + 1])
         assert (np.abs(got - p) <= BF16 * np.abs(p) + (k + 1) * U * mag).all(), (name, r)
         check_h(host(h[r:r + 1]), p, mag, k, kind, (name, r))
+        check_h(host(alone[r:r + 1]), p, mag, k, kind, (name, r))
         check_dgrad(host(dp[r:r + 1]), host(dy[r:r + 1]), host(v[e:e + 1]), host(pre[r:r + 1]), one,
                     kind, (name, r))
     # the whole, expert by expert, in fp32 on the device: far looser, but no tile is left out
@@ -243,6 +246,7 @@ def test_every_kernel(name):
         z = z * torch.sigmoid(z) if kind == "silu" else z * torch.special.ndtr(z)
         z = z * p[:, H:]
         assert (h[a:b].float() - z).norm() < 4e-3 * z.norm(), (name, e)
+        assert (alone[a:b].float() - z).norm() < 4e-3 * z.norm(), (name, e)
         q = pre[a:b].float().requires_grad_()
         act = torch.nn.functional.silu if kind == "silu" else torch.nn.functional.gelu
         d = dy[a:b].float() @ v[e].float()
