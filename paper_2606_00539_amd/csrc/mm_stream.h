@@ -34,7 +34,8 @@ class Tiles {
       const Set s = read(e0, sum);
       if (e0 == 0) first = s;
       else if (e0 == 64) second = s;
-      sum = s.before + int(lane_of(uint32_t(s.upto), 63));
+      // (offsets in order leave no more tiles than this; others would let the sum overflow)
+      sum = min(s.before + int(lane_of(uint32_t(s.upto), 63)), most());
     }
     total = sum * per;
   }
@@ -49,11 +50,12 @@ class Tiles {
       t.rows = g.rows - t.row;
       return t;
     }
+    const int vm = v / per;
     int sum = 0;
     for (int e0 = 0; e0 <= g.num; e0 += 64) {
       const Set s = e0 == 0 ? first : e0 == 64 ? second : read(e0, sum);
       const int above = s.before + s.upto;
-      const uint64_t here = __ballot((above - s.n) * per <= v && v < above * per);
+      const uint64_t here = __ballot(above - s.n <= vm && vm < above);
       if (here != 0) {
         const int src = __ffsll((unsigned long long)here) - 1;
         const int tiles_m = int(lane_of(uint32_t(s.n), src));
@@ -64,7 +66,7 @@ class Tiles {
         t.rows = int(lane_of(uint32_t(s.end), src)) - t.row;
         return t;
       }
-      sum = s.before + int(lane_of(uint32_t(s.upto), 63));
+      sum = min(s.before + int(lane_of(uint32_t(s.upto), 63)), most());
     }
     return t;
   }
@@ -83,6 +85,8 @@ class Tiles {
     s.upto = int(wave_prefix(uint32_t(s.n)));
     return s;
   }
+
+  __device__ __forceinline__ int most() const { return g.rows / kStreamM + g.num + 1; }
 
   const GroupArgs& g;
   int per, lane_;
