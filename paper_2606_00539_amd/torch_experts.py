@@ -13,7 +13,7 @@ import torch
 
 from . import torch_ops as ops
 from .binding import GNMR_BUDGET_ACTIVE, Controller, gnmr_grouped_wgrad_num_partials
-from .torch_units import clip_from_controller
+from .torch_units import clip_from_controller, clippable
 
 
 def _readable(dy):
@@ -258,7 +258,8 @@ class ExpertUnits:
     def feed_forward(self, up, down, x, offsets, activation="silu"):
         """The gated block y[t] = V_e (act(G_e x[t]) * (U_e x[t])) for the rows t of every expert e:
         matrix `up` is [G_e; U_e], [experts, 2 hidden, in], and `down` V_e, [experts, out, hidden];
-        activation "silu" or "gelu"."""
+        activation "silu" or "gelu".  As with torch's own operators, its backward pass is captured in a
+        graph only while no autograd graph made outside the capture holds the same leaves."""
         a, b = self.weights[self._index[up]], self.weights[self._index[down]]
         if a.shape[0] != b.shape[0] or a.shape[1] != 2 * b.shape[2] or b.shape[2] % 8:
             raise ValueError(f"{up} and {down} must be [experts, 2 hidden, in] and [experts, out, "
@@ -309,11 +310,12 @@ class ExpertUnits:
                      eps: float = 1e-6, stream=None):
         """step(), and then the gradients, with `others` (more gradient tensors of the step), scaled in
         place to a global norm of at most max_norm.  The units' norms are those that the step has just
-        made; only `others` are read for the norm.  Returns it (a float64 scalar on the device)."""
-        stream = self._stream(stream)
+        made; only `others`, ready on `stream`, are read for the norm.  Returns it (a float64 scalar on the
+        device).  A call that is refused for `others` has not stepped."""
+        stream, gradients = self._stream(stream), list(self.grads.values())
+        others = clippable(gradients, others, max_norm, eps, self.device)
         self.step(alpha_t, beta_t, stream)
-        return clip_from_controller(self.ctl, list(self.grads.values()), others, max_norm, eps,
-                                    stream, self.device)
+        return clip_from_controller(self.ctl, gradients, others, max_norm, eps, stream, self.device)
 
     def query(self, stream=None) -> dict:
         out = self.ctl.query(self._stream(stream))

@@ -40,6 +40,25 @@ class _DeviceNorms:
                                          "data": (int(ctl.device_outputs()["norm"]), False)}
 
 
+def clippable(gradients, others, max_norm, eps, device):
+    """`others` as a list.  What clipping them and `gradients` would refuse is refused here, before
+    the controller has stepped."""
+    import torch
+
+    others = list(others)
+    if not max_norm >= 0 or not 0 <= eps < float("inf"):
+        raise ValueError(f"max_norm must be >= 0, eps finite and >= 0, not {max_norm} and {eps}")
+    for t in others:
+        if t is None or t.dtype not in (torch.bfloat16, torch.float32) or t.device != device or \
+                not t.is_contiguous():
+            raise TypeError("others must be contiguous bf16 or fp32 tensors on the units' device")
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                   for t in (*gradients, *others) if t is not None and t.numel())
+    if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+        raise RuntimeError("a gradient overlaps another one: it would be scaled twice")
+    return others
+
+
 def clip_from_controller(ctl, gradients, others, max_norm, eps, stream, device):
     """The gradients that ctl has just stepped from, which are all of its units', and `others`
     scaled in place to a global norm of at most max_norm, on `stream`; returns the norm.  Only
@@ -53,7 +72,7 @@ def clip_from_controller(ctl, gradients, others, max_norm, eps, stream, device):
                                            device=device)
     with torch.cuda.stream(stream):
         norms = torch.as_tensor(_DeviceNorms(ctl), device=device)
-        return clip_gradients(gradients + list(others), max_norm, known=range(len(gradients)),
+        return clip_gradients(gradients + others, max_norm, known=range(len(gradients)),
                               norms=norms, eps=eps)
 
 
@@ -116,11 +135,13 @@ class TorchUnits:
         """step(), and then the units' gradients, with `others` (gradients of parameters that are no
         unit's), scaled in place to a global norm of at most max_norm.  The units' norms are those that
         the step has just made, so their gradients are read once less than by a norm of their own.
-        Returns the norm (a float64 scalar on the device)."""
-        stream = _current(stream)
+        Returns the norm (a float64 scalar on the device).  `others` are ready on `stream`, as the units'
+        gradients are; a call that is refused for them has not stepped."""
+        stream, device = _current(stream), self.params[0].device
+        gradients = [p.grad for p in self.params]
+        others = clippable(gradients, others, max_norm, eps, device)
         self.step(alpha_t, beta_t, stream)
-        return clip_from_controller(self.ctl, [p.grad for p in self.params], others, max_norm, eps,
-                                    stream, self.params[0].device)
+        return clip_from_controller(self.ctl, gradients, others, max_norm, eps, stream, device)
 
     def query(self, stream=None) -> dict:
         out = self.ctl.query(_current(stream))
@@ -316,10 +337,11 @@ class FusedWgradUnits:
         place to a global norm of at most max_norm.  The weights' norms are those that the step has
         just made: their gradients are not read for it.  Returns the norm (a float64 scalar on the
         device)."""
-        stream = _current(stream)
+        stream, device = _current(stream), self.modules[0].weight.device
+        gradients = [m.weight.grad for m in self.modules]
+        others = clippable(gradients, others, max_norm, eps, device)
         self.step(alpha_t, beta_t, stream)
-        return clip_from_controller(self.ctl, [m.weight.grad for m in self.modules], others, max_norm,
-                                    eps, stream, self.modules[0].weight.device)
+        return clip_from_controller(self.ctl, gradients, others, max_norm, eps, stream, device)
 
     def query(self, stream=None) -> dict:
         out = self.ctl.query(_current(stream))

@@ -117,3 +117,78 @@ def test_refusals(block):
             units.feed_forward(a, b, x, OFF)
     with pytest.raises(KeyError):
         units.feed_forward("up", "other", x, OFF)
+
+
+def test_one_matrix_as_both(monkeypatch):
+    """[experts, 2 hidden, hidden] is up and down at once: its gradient is the sum of both."""
+    C.patch(monkeypatch)
+    monkeypatch.setattr(E.ops, "gated_linear", gated_linear)
+    monkeypatch.setattr(E.ops, "gated_dgrad", gated_dgrad)
+    w = C.weight(3, 2 * H, H)
+    units = E.ExpertUnits([("m", w)], low_cost=False)
+    g = torch.Generator().manual_seed(4)
+    x = torch.randn(8, H, generator=g).to(torch.bfloat16).requires_grad_()
+    dy = torch.randn(8, 2 * H, generator=g).to(torch.bfloat16)
+    units.feed_forward("m", "m", x, OFF).backward(dy)
+    leaves = [t.detach().as_subclass(torch.Tensor).float().requires_grad_() for t in (x, w)]
+    reference(leaves[0], leaves[1], leaves[1]).backward(dy.float())
+    for got, ref in ((x.grad, leaves[0].grad), (units.grads["m"], leaves[1].grad)):
+        assert (got.float() - ref).norm() < 5 * 2.0 ** -8 * ref.norm()
+
+
+class Steps:
+    def __init__(self):
+        self.steps = 0
+
+    def step(self, *a, **kw):
+        self.steps += 1
+
+    step_from_partials = step
+
+
+def bad_others(grad):
+    f = torch.zeros(12)
+    return [([None], TypeError), ([f.half()], TypeError), ([f.view(3, 4).t()], TypeError),
+            ([f.to("meta")], TypeError), ([f, f], RuntimeError), ([f[:8], f[4:]], RuntimeError),
+            ([grad], RuntimeError), ([grad.view(-1)[3:5]], RuntimeError)]
+
+
+def check_step_clipped(units, grad, step):
+    """What clipping refuses is refused before the controller has stepped."""
+    for others, error in bad_others(grad):
+        with pytest.raises(error):
+            units.step_clipped(1.1, 1.5, 1.0, others=others)
+    for kw in ({"max_norm": -1.0}, {"max_norm": float("nan")}, {"max_norm": 1.0, "eps": -1.0},
+               {"max_norm": 1.0, "eps": float("inf")}):
+        with pytest.raises(ValueError):
+            units.step_clipped(1.1, 1.5, **kw)
+    assert step.steps == 0
+
+
+def test_a_refused_step_clipped_has_not_stepped(block, monkeypatch):
+    units, x, up, down = block
+    units.feed_forward("up", "down", x, OFF).float().sum().backward()
+    units.device, units.ctl = torch.device("cpu"), Steps()
+    check_step_clipped(units, units.grads["up"], units.ctl)
+    assert units._filled == [True, True]
+    clipped = []
+    monkeypatch.setattr(E, "clip_from_controller", lambda *a: clipped.append(a))
+    other = torch.ones(3)
+    units.step_clipped(1.1, 1.5, 1.0, others=(t for t in [other]))
+    assert units.ctl.steps == 1 and clipped[0][1:3] == (list(units.grads.values()), [other])
+
+
+@pytest.mark.parametrize("kind", ["TorchUnits", "FusedWgradUnits"])
+def test_a_refused_step_clipped_of_other_units_has_not_stepped(kind, monkeypatch):
+    from paper_2606_00539_amd import torch_units as U
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: C.TheStream)
+    units = object.__new__(getattr(U, kind))
+    m = torch.nn.Linear(4, 3)
+    m.weight.grad = torch.ones(3, 4)
+    units.modules, units.params, units.param_names, units.ctl = [m], [m.weight], ["w"], Steps()
+    units._produced, units.partials = [m.weight.grad.data_ptr()], None
+    check_step_clipped(units, m.weight.grad, units.ctl)
+    monkeypatch.setattr(U, "clip_from_controller", lambda *a: None)
+    units.step_clipped(1.1, 1.5, 1.0, others=[torch.ones(3)])
+    assert units.ctl.steps == 1

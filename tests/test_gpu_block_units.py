@@ -326,6 +326,35 @@ def test_fused_wgrad_units_step_clipped():
     units.close()
 
 
+def test_torch_units_step_clipped_in_a_graph():
+    """Captured with the controller's step, and replayed with the program's own work between."""
+    torch = require_gpu()
+    from paper_2606_00539_amd.torch_units import TorchUnits
+
+    g = torch.Generator(device="cuda").manual_seed(11)
+    made = [[torch.randn(40, 72, generator=g, device="cuda") * 2.0 ** k,
+             torch.randn(77, generator=g, device="cuda")] for k in range(4)]
+    p = torch.nn.Parameter(torch.zeros(40, 72, device="cuda"))
+    p.grad, other = made[0][0].clone(), made[0][1].clone()
+    units = TorchUnits([("w", p)], max_o=1, lock_len=1)
+    units.step_clipped(1.1, 1.5, 20.0, others=[other])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = units.step_clipped(1.1, 1.5, 20.0, others=[other])
+    for big, small in made:
+        p.grad.copy_(big)
+        other.copy_(small)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        norm = float((big.double().square().sum() + small.double().square().sum()).sqrt())
+        assert abs(float(got) - norm) <= 1e-5 * norm
+        assert scaled(p.grad, big, 20.0 / norm) and scaled(other, small, 20.0 / norm)
+        np.testing.assert_allclose(units.query()["norm"], float(big.double().norm()), rtol=1e-5)
+    units.close()
+
+
 # -- a block ----------------------------------------------------------------------------
 
 def test_a_block_of_them_together():

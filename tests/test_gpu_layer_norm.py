@@ -332,6 +332,43 @@ def test_module(dtype, wtype):
     nobias(x).sum().backward()
 
 
+def test_module_in_a_graph():
+    """Forward and backward captured after a warm-up on another stream; weights' gradients and all."""
+    torch, _ = ops()
+    from paper_2606_00539_amd.torch_layers import LayerNorm
+
+    say("LayerNorm module, graph")
+    x, dy, w, b = data(30, 136, 12, "bf16", "f32")
+    m = LayerNorm(136)
+    with torch.no_grad():
+        m.weight.copy_(w)
+        m.bias.copy_(b)
+    xt = x.clone().requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        m(xt).backward(dy)
+    torch.cuda.current_stream().wait_stream(side)
+    xt.grad = m.weight.grad = m.bias.grad = None
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = m(xt)
+        y.backward(dy)
+    from paper_2606_00539_amd import torch_ops as t
+    for k in range(4):
+        with torch.no_grad():
+            xt.mul_(-1.25)
+        dy.add_(0.25)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want, mean, rstd = t.layer_norm(xt.detach(), w, b)
+        grads = t.layer_norm_backward(dy, xt.detach(), mean, rstd, w, bias=True)
+        for p, q in zip((y, xt.grad, m.weight.grad, m.bias.grad), (want, *grads)):
+            assert torch.equal(p, q), k
+
+
 def test_module_gradients_against_differences():
     torch, _ = ops()
     from paper_2606_00539_amd.torch_layers import layer_norm
