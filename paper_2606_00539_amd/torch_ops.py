@@ -28,6 +28,7 @@ from . import binding as B
 _DTYPES = {torch.bfloat16: B.GNMR_BF16, torch.float32: B.GNMR_F32}
 _num_partials = functools.lru_cache(None)(B.gnmr_grouped_wgrad_num_partials)
 _clip_workspace = functools.lru_cache(None)(B.gnmr_clip_gradients_workspace)
+_norm_workspace = functools.lru_cache(1024)(B.gnmr_layer_norm_backward_workspace)
 _ACTIVATIONS = {"silu": B.GNMR_ACT_SILU, "gelu": B.GNMR_ACT_GELU}
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
@@ -412,7 +413,7 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, bias=False, input_grad=T
         db = torch.empty(cols, dtype=type_, device=where)
     rows, n = xs.shape[0], 0
     if dw is not None or db is not None:
-        n = B.gnmr_layer_norm_backward_workspace(rows, cols)
+        n = _norm_workspace(rows, cols)
         if n:
             work = torch.empty(n, dtype=torch.uint8, device=where)
     device, stream = _on(x)
