@@ -235,9 +235,12 @@ inline int grouped_tile(const GroupArgs& g, int N, int K, int weight, double bes
 
 // Tiles of products one after the other on a CU (mm_stream.h), and whether that is the way for a
 // product of grouped rows, `bytes` of memory to each value of whose result are read and written at its
-// tiles' ends.  A step takes 0.70 us, the end of a tile 7 and its bytes 32 KB to a us; us that
-// were measured, and in tiles of the best edge: 24,576 rows in 64 groups, 2048 to 2 x 1408 (3 bytes)
-// 360 and 402, the gradient (8 bytes) 226 and 239; 8,192 rows, 4096 to 2 x 11008 1,195 and 1,150.
+// tiles' ends.  A call takes 4 us, a step 0.70 and the bytes of a tile's end 64 KB to a us: fitted to 65
+// shapes (300 to 65,536 rows, up to 128 groups, K 256 to 4096), for 15 of whose 195 calls the slower way is
+// taken by 5 to 10%, for the others by less or not at all.  us one after the other, and in tiles of the
+// best edge: 24,640 rows in 64 groups, 2048 to 2 x 1408, both products and h (3 bytes) 344 and 423, h alone
+// (1) 320 and 344, the gradient (8) 222 and 235; 5,000 rows in 64 groups, 4096 to 2 x 2752, 573 and 749;
+// 9,000 rows in 8 groups, 320 to 2 x 688, 20.8 and 24.8; 8,192 rows, 4096 to 2 x 11008, 1,151 and 1,103.
 constexpr int kStreamM = 128, kStreamN = 256;
 inline bool streams(const GroupArgs& g, int N, int K, double beside, double bytes) {
   if (K % 64 != 0 || K < 256) return false;     // (whole steps, two rounds of three at least)
@@ -247,7 +250,7 @@ inline bool streams(const GroupArgs& g, int N, int K, double beside, double byte
   const double tiles = ceil(double(g.rows) / kStreamM + (g.offsets == nullptr ? 0.0 : 0.5 * used)) *
                        ceil(double(N) / kStreamN);
   const double steps = ceil(K / 192.0) * 3.0;
-  return ceil(tiles / 256.0) * (0.70 * steps + 7.0 + kStreamM * kStreamN * bytes / 32e3) < tiles_us;
+  return 4.0 + ceil(tiles / 256.0) * (0.70 * steps + kStreamM * kStreamN * bytes / 64e3) < tiles_us;
 }
 
 // The launches of a batch of products of K8: X X^T and A A, symmetric (tiles on and above the
@@ -309,9 +312,6 @@ inline RowLaunch row_launch(const GroupArgs& g, int N, int K, int weight, double
 
 // Bytes that a value of the gated gradient's product costs beside its own: two of p are read, and two written.
 constexpr double kGatedDgradBeside = 6.0;
-inline bool gated_linear_streams(const GroupArgs& g, int H, int K, bool keep) {
-  return streams(g, 2 * H, K, keep ? 1.0 : 0.0, keep ? 3.0 : 1.0);
-}
 inline bool gated_dgrad_streams(const GroupArgs& g, int H, int K) {
   return streams(g, H, K, kGatedDgradBeside, kGatedDgradBeside + 2.0);
 }
@@ -321,6 +321,12 @@ inline bool gated_dgrad_streams(const GroupArgs& g, int H, int K) {
 // caches: 64 experts 2048 x 1408, 48 rows 85 and 77.5, 1,536 rows 146 and 133; 8 of 4096 x 11008, 64
 // rows 249 and 223 (6.5 TB/s).
 inline bool gated_weights_once(const GroupArgs& g) { return g.rows <= 64 * int64_t(g.num); }
+
+// (Weights that are read once: tiles of 64.  4,096 rows in 64 groups, 2048 to 2 x 1408, us: 163 in them
+// and 176 one after the other; 2,048 rows 156 and 177.)
+inline bool gated_linear_streams(const GroupArgs& g, int H, int K, bool keep) {
+  return !gated_weights_once(g) && streams(g, 2 * H, K, keep ? 1.0 : 0.0, keep ? 3.0 : 1.0);
+}
 
 // Makes them: launch(edge, share, workgroups), with *tiles_n set.
 template <class Launch>

@@ -11,6 +11,11 @@
 //
 // bf16 operands, fp32 sums and formulas, one rounding of each result: neither p (where it is not
 // kept) nor d goes to memory.
+//
+// Bounds and times: a token's experts' weights for few rows (48 rows in 35 of 64 experts, 2048 to 2 x 1408:
+// 404 MB in 78 us, 5.2 TB/s); the chip's power in 256 tiles for many (8,192 rows, 4096 to 2 x 11008: 1,106
+// us, 1,340 TFLOP/s); weights from memory and the ends of ragged groups between them (24,576 rows in 64
+// experts, 2048 to 2 x 1408 with p: 343 us, 830 TFLOP/s; its gradient 215 us).
 #include <type_traits>
 
 #include "gnmr_internal.h"

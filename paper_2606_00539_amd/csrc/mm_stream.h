@@ -9,6 +9,11 @@
 // tiles, of two steps each in LDS, takes as long as a workgroup to a tile where groups are large (the
 // chip's power bounds both), and longer where they are ragged: 24,576 rows in 64 groups, 2048 to 2 x
 // 1408, us: 128 tiles 402, 256 tiles 409, 128 x 256 ones like this 360, 256 ones like this 462.
+//
+// What bounds them: where groups are many, weights that come from memory while two steps (96 KB a CU) are
+// under way (as many rows in 64 groups take 302 us, in 8 groups 230, h alone); there is no LDS for more. A
+// tile's results sent out piece by piece during the next one's first steps change nothing (317 and 316 us h
+// alone; with the products the registers do not hold both).
 #pragma once
 
 #include "groups.h"

@@ -72,8 +72,10 @@ SHAPES = {
                                                     ("256 all", "256 rounds and rest")),
     "streams, 70 experts": (1000, 2048, loads(70, 9000, 9), 300, ("stream", "stream")),
     "streams, 4 experts": (5504, 4096, loads(4, 1000, 10), 5, ("stream", "stream")),
-    "stream of the gradient, one expert": (4096, 4096, None, 4093, ("256 all", "stream")),
-    "stream, one expert": (5504, 2048, None, 2041, ("stream", "256 all")),
+    "streams, one expert": (4096, 4096, None, 4093, ("stream", "stream")),
+    "streams, one expert of fewer rows": (5504, 2048, None, 2041, ("stream", "stream")),
+    "streams of four steps": (2000, 256, None, 3001, ("stream", "stream")),
+    "streams of five steps, 20 experts": (1000, 320, loads(20, 3000, 11), 40, ("stream", "stream")),
     "stream of the gradient, fewer than 256 tiles": (2752, 4096, None, 2000, ("256 all", "stream")),
     "rounds and rest, one expert": (1912, 5128, None, 10115, ("256 rounds and rest", "128 all")),
 }
