@@ -9,6 +9,10 @@
 // much larger than the deviations its rounding alone would show in x - m; the gradients' kernel does
 // the same with the mean that it is given.  Both kernels take rows by turns, weights in registers and
 // the next row on its way; the gradients' keeps its columns' sums over its rows in registers too.
+//
+// Bound by the rows' bytes.  42M values, TB/s of forward and gradients: fp32 6.0 to 6.5 and 5.3 to 6.0 at widths
+// from 768 to 11,008 (odd ones 4.8 and 5.5), bf16 3.7 to 4.6 and 3.4 to 4.9 (odd ones 3.4 and 2.4), where the
+// conversions and the gradients' sums take as long as the bytes.
 #include <algorithm>
 
 #include "gnmr_internal.h"
@@ -20,11 +24,14 @@ namespace {
 
 // How a row is held: by kLanes lanes of a wavefront (8 to 64, several rows to a wavefront or
 // workgroup), or, kWide, by all lanes of `waves` wavefronts, as many as it needs; kEight runs of eight
-// bf16 values (twice as many of four fp32 ones) to a lane.  kExact: cols fills all of them.
+// bf16 values (twice as many of four fp32 ones) to a lane.  kFill: what cols fills of them, kAll (kExact),
+// kWhole runs, or one of them in part.
 // kPast: the result is written past the caches.
-template <bool kIsF32, int kLaneCount, bool kIsWide, int kEight, bool kIsExact, bool kIsPast = false>
+enum Fill { kPart, kWhole, kAll };
+template <bool kIsF32, int kLaneCount, bool kIsWide, int kEight, int kFilled, bool kIsPast = false>
 struct Shape {
-  static constexpr bool kF32 = kIsF32, kWide = kIsWide, kExact = kIsExact, kPast = kIsPast;
+  static constexpr bool kF32 = kIsF32, kWide = kIsWide, kExact = kFilled == kAll, kPast = kIsPast;
+  static constexpr int kFill = kFilled;
   static constexpr int kLanes = kLaneCount, N = kF32 ? 4 : 8, kRuns = kF32 ? 2 * kEight : kEight;
   static constexpr int kBytes = kF32 ? 4 : 2;
   static constexpr int kMost = kEight == 4 ? 8 : 16;   // wavefronts to a workgroup
@@ -39,26 +46,46 @@ template <class S>
 struct Place {
   int slot, at, lanes;
   int cols;
+  int ragged;   // the run that one lane has in part, or -1
 
   __device__ __forceinline__ Place(int waves, int cols_) : cols(cols_) {
     lanes = S::kWide ? 64 * waves : S::kLanes;
     slot = threadIdx.x / lanes;
     at = threadIdx.x % lanes;
+    ragged = cols % S::N != 0 ? cols / S::N / lanes : -1;
   }
   __device__ __forceinline__ int col(int i) const { return S::N * (at + i * lanes); }
   // values of run i that exist
   __device__ __forceinline__ int count(int i) const { return S::kExact ? S::N : cols - col(i); }
-  __device__ __forceinline__ bool is(int i, int k) const { return S::kExact || col(i) + k < cols; }
+  __device__ __forceinline__ bool is(int i, int k) const {
+    return S::kExact || col(i) + (S::kFill == kWhole ? 0 : k) < cols;
+  }
 
+  // Run i as it lies in memory, in one access whatever of it exists (a branch around loads of single
+  // values would wait for them there): a run past the row's end is the row's last N values.
   template <bool kPast>
   __device__ __forceinline__ Raw<S::kF32, S::N> load(const char* row, int i) const {
     if constexpr (S::kExact) return load_raw<S::kF32, S::N, kPast>(row, col(i));
-    else return load_raw_some<S::kF32, S::N>(row, col(i), count(i));
+    if (S::kFill == kPart && cols < S::N) return load_raw_some<S::kF32, S::N>(row, col(i), count(i));
+    return load_raw<S::kF32, S::N, kPast>(row, min(col(i), cols - S::N));
+  }
+  // its values; those that do not exist are others
+  __device__ __forceinline__ Run<S::N> values(const Raw<S::kF32, S::N>& raw, int i) const {
+    Run<S::N> e = raw.values();
+    if (S::kFill == kPart && i == ragged && cols >= S::N) {
+      const int n = count(i), by = n > 0 && n < S::N ? S::N - n : 0;    // that it was read too early
+#pragma unroll
+      for (int step = S::N / 2; step > 0; step /= 2)
+#pragma unroll
+        for (int k = 0; k + step < S::N; ++k)
+          if (by & step) e.v[k] = e.v[k + step];
+    }
+    return e;
   }
   template <bool kPast>
   __device__ __forceinline__ void store(char* row, int i, const Run<S::N>& e) const {
-    if constexpr (S::kExact) store_run<S::kF32, S::N, kPast>(row, col(i), e);
-    else if (count(i) > 0) store_some<S::kF32, S::N>(row, col(i), count(i), e);
+    if (S::kExact || count(i) >= S::N) store_run<S::kF32, S::N, kPast>(row, col(i), e);
+    else if (S::kFill == kPart && count(i) > 0) store_some<S::kF32, S::N>(row, col(i), count(i), e);
   }
   // run i of the weights or the biases, of either type, or ones or zeros
   __device__ __forceinline__ Run<S::N> weights(const void* w, bool f32, int i, float none) const {
@@ -140,9 +167,9 @@ __global__ __launch_bounds__(S::kWide ? 1024 : kThreads) void k10_forward(const 
     float s[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < S::kRuns; ++i) {
-      v[i] = next[i].values();
+      v[i] = p.values(next[i], i);
 #pragma unroll
-      for (int k = 0; k < S::N; ++k) s[0] += v[i].v[k];
+      for (int k = 0; k < S::N; ++k) s[0] += p.is(i, k) ? v[i].v[k] : 0.0f;
     }
     if (first + turn < a.rows) request(row + turn);
     row_sums<S, 1>(s, a.waves, red[0]);
@@ -217,11 +244,13 @@ __global__ __launch_bounds__(S::kWide ? 64 * S::kMost : kThreads) void k10_backw
     float s[3] = {0.0f, 0.0f, 0.0f};    // of x - mean, g, g (x - mean)
 #pragma unroll
     for (int i = 0; i < S::kRuns; ++i) {
-      v[i] = next_x[i].values();
-      g[i] = next_g[i].values();
+      v[i] = p.values(next_x[i], i);
+      g[i] = p.values(next_g[i], i);
 #pragma unroll
       for (int k = 0; k < S::N; ++k) {
-        const float d = p.is(i, k) ? v[i].v[k] - mean : 0.0f, q = g[i].v[k] * w[i].v[k];
+        const float d = p.is(i, k) ? v[i].v[k] - mean : 0.0f;
+        g[i].v[k] = p.is(i, k) ? g[i].v[k] : 0.0f;
+        const float q = g[i].v[k] * w[i].v[k];
         v[i].v[k] = d;
         s[0] += d;
         s[1] += q;
@@ -305,16 +334,17 @@ __global__ __launch_bounds__(64 * kReduceWaves) void k10_reduce(const LayerNormB
   else store_one<false>(out, col, s);
 }
 
-// launch(lanes, wide, eight, exact): the shape of rows of that many columns.  8192 x 5120 bf16, two
+// launch(lanes, wide, eight, fill): the shape of rows of that many columns.  8192 x 5120 bf16, two
 // runs to a lane of five wavefronts: 34 us; one run to ten: 65.  The gradients of 8191 x 4096, one
-// run to eight wavefronts: 45 us; two to four: 47.5.
-template <bool kBackward, bool kExact, class Launch>
+// run to eight wavefronts: 45 us; two to four: 47.5.  20480 x 2048 bf16, two runs to two wavefronts and,
+// gradients, one to four: 37 and 53 us; four runs to one wavefront 63 and 63.
+template <bool kBackward, int kFill, class Launch>
 void by_width(int cols, Launch&& launch) {
   using std::integral_constant;
   using std::bool_constant;
   constexpr int kWave = 512;    // columns that a wavefront holds with one run of eight to a lane
   auto of = [&](auto lanes, auto wide, auto eight) {
-    launch(lanes, wide, eight, bool_constant<kExact>{});
+    launch(lanes, wide, eight, integral_constant<int, kFill>{});
   };
   const bool_constant<false> narrow;
   const bool_constant<true> wide;
@@ -327,10 +357,12 @@ void by_width(int cols, Launch&& launch) {
   const integral_constant<int, 64> all;
   if (cols <= kWave) return of(all, narrow, one);
   if (cols <= 2 * kWave) return of(all, narrow, two);
-  if (cols <= 4 * kWave) return of(all, narrow, four);
-  if constexpr (!kBackward) return of(all, wide, two);
-  else if (cols <= 16 * kWave) return of(all, wide, one);
-  else return of(all, wide, four);
+  if constexpr (!kBackward) {
+    of(all, wide, two);
+  } else {
+    if (cols <= 16 * kWave) return of(all, wide, one);
+    of(all, wide, four);
+  }
 }
 
 // Who holds a row: wavefronts to one (1: or a part of it), rows that a workgroup takes at a time, and
@@ -342,7 +374,7 @@ struct Held {
 template <bool kBackward>
 Held held(int cols) {
   Held r{};
-  by_width<kBackward, false>(cols, [&](auto lanes, auto wide, auto eight, auto) {
+  by_width<kBackward, kPart>(cols, [&](auto lanes, auto wide, auto eight, auto) {
     constexpr int kPer = 8 * decltype(lanes)::value * decltype(eight)::value;
     if (decltype(wide)::value) {
       r.waves = (cols + kPer - 1) / kPer;
@@ -357,6 +389,15 @@ Held held(int cols) {
   return r;
 }
 
+// by_width with what the columns fill of its shape.  Rows of whole runs need one comparison to a run: the
+// gradients of 54613 x 768 bf16 73.6 us as rows of runs in part, 57.6 so.
+template <bool kBackward, class Launch>
+void by_fill(const Held& h, int cols, bool f32, Launch&& launch) {
+  if (h.exact) by_width<kBackward, kAll>(cols, launch);
+  else if (cols % (f32 ? 4 : 8) == 0) by_width<kBackward, kWhole>(cols, launch);
+  else by_width<kBackward, kPart>(cols, launch);
+}
+
 }  // namespace
 
 // Workgroups whose sums over their rows are added in the end: one to a CU, or as many as have 64 rows each,
@@ -364,9 +405,9 @@ Held held(int cols) {
 // 1024 fp32 15.8 and 20.3, 16384 x 1024 bf16 25.7 and 29.1; 65536 x 512 fp32 73.1 and 70.7, 100000 x 128
 // fp32 33.2 and 32.1.
 int layer_norm_parts(int64_t rows, int cols) {
-  const int per = held<true>(cols).rows;
-  const int64_t most = std::min<int64_t>(rows / 64, std::min(1024, (1 << 20) / cols));
-  return int(std::min<int64_t>((rows + per - 1) / per, std::max<int64_t>(256, most)));
+  const Held h = held<true>(cols);
+  const int64_t most = h.waves > 1 ? 256 : std::min<int64_t>(rows / 64, std::min(1024, (1 << 20) / cols));
+  return int(std::min<int64_t>((rows + h.rows - 1) / h.rows, std::max<int64_t>(256, most)));
 }
 
 hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s) {
@@ -375,17 +416,18 @@ hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s) {
   const int64_t turns = (a.rows + h.rows - 1) / h.rows;
   // 8192 x 5120 bf16, us, through and past the caches: 39.9 and 34.2 (where they could hold them, what
   // reads the rows next gains more)
-  const bool past = h.exact && a.rows * a.cols * (f32 ? 4 : 2) > int64_t(32) << 20;
-  auto launch = [&](auto lanes, auto wide, auto eight, auto exact) {
-    constexpr bool kWide = decltype(wide)::value, kExact = decltype(exact)::value;
+  const bool past = a.rows * a.cols * (f32 ? 4 : 2) > int64_t(32) << 20;
+  auto launch = [&](auto lanes, auto wide, auto eight, auto fill) {
+    constexpr bool kWide = decltype(wide)::value;
+    constexpr int kFill = decltype(fill)::value;
     const dim3 block(kWide ? 64 * h.waves : kThreads);
     // 16 wavefronts to a CU, eight workgroups of several rows (8192 x 5120: with 24 wavefronts 50 us
     // instead of 40)
     const dim3 grid{unsigned(std::min<int64_t>(turns, 256 * (kWide ? std::max(1, 16 / h.waves) : 8)))};
     auto of = [&](auto type, auto beyond) {
       hipLaunchKernelGGL((k10_forward<Shape<decltype(type)::value, decltype(lanes)::value, kWide,
-                                            decltype(eight)::value, kExact,
-                                            kExact && decltype(beyond)::value>>),
+                                            decltype(eight)::value, kFill,
+                                            decltype(beyond)::value>>),
                          grid, block, 0, s, a);
     };
     auto with = [&](auto type) {
@@ -395,8 +437,7 @@ hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s) {
     if (f32) with(std::true_type{});
     else with(std::false_type{});
   };
-  if (h.exact) by_width<false, true>(a.cols, launch);
-  else by_width<false, false>(a.cols, launch);
+  by_fill<false>(h, a.cols, f32, launch);
   return hipGetLastError();
 }
 
@@ -404,20 +445,19 @@ hipError_t launch_layer_norm_backward(LayerNormBackward a, bool f32, hipStream_t
   const Held h = held<true>(a.cols);
   a.waves = h.waves;
   a.num_parts = layer_norm_parts(a.rows, a.cols);
-  auto launch = [&](auto lanes, auto wide, auto eight, auto exact) {
+  auto launch = [&](auto lanes, auto wide, auto eight, auto fill) {
     constexpr bool kWide = decltype(wide)::value;
     const dim3 block(kWide ? 64 * h.waves * h.rows : kThreads), grid{unsigned(a.num_parts)};
     auto of = [&](auto type) {
       hipLaunchKernelGGL((k10_backward<Shape<decltype(type)::value, decltype(lanes)::value, kWide,
-                                             decltype(eight)::value, decltype(exact)::value>>),
+                                             decltype(eight)::value, decltype(fill)::value>>),
                          grid, block, 0, s, a);
     };
     if (f32) of(std::true_type{});
     else of(std::false_type{});
   };
   if (a.rows > 0) {
-    if (h.exact) by_width<true, true>(a.cols, launch);
-    else by_width<true, false>(a.cols, launch);
+    by_fill<true>(h, a.cols, f32, launch);
   }
   if (a.dweight != nullptr || a.dbias != nullptr)
     hipLaunchKernelGGL(k10_reduce, dim3(unsigned(2 * ((a.cols + 63) / 64))),

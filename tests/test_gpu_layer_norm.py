@@ -71,7 +71,10 @@ SHAPES = [(1, 1, 0, 0), (5, 2, 1, 0), (3, 7, 0, 0), (9, 8, 3, 5), (33, 63, 0, 0)
           (5, 1025, 1, 1), (3, 2048, 0, 0), (2, 2049, 0, 3), (3, 4096, 8, 0), (2, 4097, 0, 0),
           (1, 5120, 0, 0), (2, 5121, 7, 0), (3, 6144, 0, 0), (2, 6145, 0, 0), (2, 8192, 0, 0),
           (2, 8193, 0, 1), (2, 12288, 0, 0), (1, 12289, 0, 0), (1, 16383, 0, 0), (2, 16384, 0, 0),
-          (1500, 40, 0, 0), (2700, 520, 0, 0), (600, 2056, 0, 8)]
+          (1500, 40, 0, 0), (2700, 520, 0, 0), (600, 2056, 0, 8),
+          # whole runs that do not fill their lanes, by four and by eight values
+          (33, 104, 0, 0), (17, 204, 0, 4), (9, 392, 8, 0), (5, 1540, 0, 0), (1300, 2044, 4, 0),
+          (3, 4456, 0, 0), (2, 11008, 0, 0), (700, 12300, 0, 1)]
 
 
 def data(rows, cols, seed, dtype, wtype):
@@ -267,6 +270,23 @@ def test_many_rows():
     for at in (slice(0, 3), slice(rows - 3, rows)):
         check_backward(big[at], big[at], ones, dx[at], None, None)
     assert torch.equal(dx[3], dx[rows - 4]) and torch.equal(y[3], y[rows - 4])
+
+
+@pytest.mark.parametrize("cols", [4096, 4104, 4108, 4099, 1000, 203])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_results_past_the_caches(cols, dtype):
+    """Results of more than 32 MB are written past the caches: the same as those of its parts."""
+    torch, t = ops()
+    rows = (17 << 20) // cols + 5
+    say("layer norm past the caches", cols, dtype)
+    x, _, w, b = data(rows, cols, 13, dtype, "f32")
+    whole = t.layer_norm(x, w, b)
+    for k in range(0, rows, rows // 5):
+        at = slice(k, k + rows // 5)
+        for p, q in zip(whole, t.layer_norm(x[at], w, b)):
+            assert torch.equal(p[at], q)
+    for at in (slice(0, 3), slice(rows - 3, rows)):
+        check_forward(x[at], w, b, *(p[at] for p in whole))
 
 
 def test_graph_replays_and_another_stream():
