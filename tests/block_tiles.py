@@ -74,6 +74,7 @@ SHAPES = {
     "streams, 4 experts": (5504, 4096, loads(4, 1000, 10), 5, ("stream", "stream")),
     "streams, one expert": (4096, 4096, None, 4093, ("stream", "stream")),
     "streams, one expert of fewer rows": (5504, 2048, None, 2041, ("stream", "stream")),
+    "streams, 200 experts": (200, 256, loads(200, 25000, 12), 77, ("stream", "stream")),
     "streams of four steps": (2000, 256, None, 3001, ("stream", "stream")),
     "streams of five steps, 20 experts": (1000, 320, loads(20, 3000, 11), 40, ("stream", "stream")),
     "stream of the gradient, fewer than 256 tiles": (2752, 4096, None, 2000, ("256 all", "stream")),
