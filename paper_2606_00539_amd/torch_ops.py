@@ -25,6 +25,7 @@ import torch
 
 from . import binding as B
 
+_T = torch.Tensor
 _DTYPES = {torch.bfloat16: B.GNMR_BF16, torch.float32: B.GNMR_F32}
 _num_partials = functools.lru_cache(None)(B.gnmr_grouped_wgrad_num_partials)
 _clip_workspace = functools.lru_cache(None)(B.gnmr_clip_gradients_workspace)
@@ -451,9 +452,9 @@ def clip_gradients(gradients, max_norm, out=None, known=(), norms=None, eps=1e-6
 
     def types(name, tensors):
         kinds = [_DTYPES.get(t.dtype) for t in tensors]
-        if None in kinds or not all([t.is_contiguous() for t in tensors]) or not like.is_cuda:
+        if None in kinds or not all(map(_T.is_contiguous, tensors)) or not like.is_cuda:
             raise TypeError(f"every {name} must be a contiguous bf16 or fp32 tensor on a HIP device")
-        if [t.device for t in tensors].count(device) != count:
+        if list(map(_T.get_device, tensors)).count(device.index) != count:
             raise ValueError("all gradients must be on one device")
         return kinds
     kinds = out_kinds = types("gradient", gradients)
@@ -461,7 +462,7 @@ def clip_gradients(gradients, max_norm, out=None, known=(), norms=None, eps=1e-6
         out_kinds = types("out", outs)
         if any([o.shape != g.shape for g, o in zip(gradients, outs)]):
             raise ValueError("every out must have its gradient's shape")
-    table = list(zip(gradients, outs, [g.numel() for g in gradients], kinds, out_kinds,
+    table = list(zip(gradients, outs, map(_T.numel, gradients), kinds, out_kinds,
                      [k in known for k in range(count)] if known else [0] * count))
     norm = torch.empty((), dtype=torch.float64, device=device)
     n = _clip_workspace(count)
