@@ -235,7 +235,9 @@ gnmr_status gnmr_layer_norm(const void* x, int32_t x_dtype, int64_t x_stride, co
 
 int64_t gnmr_layer_norm_backward_workspace(int64_t rows, int32_t cols) {
   if (rows <= 0 || cols <= 0 || cols > kLayerNormCols) return 0;
-  return int64_t(layer_norm_parts(rows, cols)) * 2 * cols * 4;
+  // (for either type)
+  return int64_t(std::max(layer_norm_parts(rows, cols, true), layer_norm_parts(rows, cols, false))) *
+         2 * cols * 4;
 }
 
 gnmr_status gnmr_layer_norm_backward(const void* dy, int64_t dy_stride, const void* x,

@@ -315,7 +315,7 @@ struct LayerNormBackward {
   int32_t num_parts, waves;   // set by the launch
 };
 // Workgroups whose sums make the gradients of weight and bias.
-int layer_norm_parts(int64_t rows, int cols);
+int layer_norm_parts(int64_t rows, int cols, bool f32);
 hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s);
 hipError_t launch_layer_norm_backward(LayerNormBackward a, bool f32, hipStream_t s);
 

@@ -338,8 +338,12 @@ __global__ __launch_bounds__(64 * kReduceWaves) void k10_reduce(const LayerNormB
 // runs to a lane of five wavefronts: 34 us; one run to ten: 65.  The gradients of 8191 x 4096, one
 // run to eight wavefronts: 45 us; two to four: 47.5.  20480 x 2048 bf16, two runs to two wavefronts and,
 // gradients, one to four: 37 and 53 us; four runs to one wavefront 63 and 63.
+//
+// The gradients of bf16 rows that fill two runs of their wavefronts have them where more wavefronts then
+// find a place among the workgroup's 16: 8192 x 5120, five to a row and three rows, 56 us; ten and one
+// 67.  (Of fp32 they would need more registers than there are: 141 and 84.)
 template <bool kBackward, int kFill, class Launch>
-void by_width(int cols, Launch&& launch) {
+void by_width(int cols, bool f32, Launch&& launch) {
   using std::integral_constant;
   using std::bool_constant;
   constexpr int kWave = 512;    // columns that a wavefront holds with one run of eight to a lane
@@ -360,6 +364,11 @@ void by_width(int cols, Launch&& launch) {
   if constexpr (!kBackward) {
     of(all, wide, two);
   } else {
+    auto used = [](int waves) { return waves * (16 / waves); };
+    if constexpr (kFill == kAll)
+      if (!f32 && cols <= 16 * kWave && cols % (2 * kWave) == 0 &&
+          used(cols / (2 * kWave)) > used(cols / kWave))
+        return of(all, wide, two);
     if (cols <= 16 * kWave) return of(all, wide, one);
     of(all, wide, four);
   }
@@ -372,9 +381,9 @@ struct Held {
   bool exact;
 };
 template <bool kBackward>
-Held held(int cols) {
+Held held(int cols, bool f32) {
   Held r{};
-  by_width<kBackward, kPart>(cols, [&](auto lanes, auto wide, auto eight, auto) {
+  by_width<kBackward, kAll>(cols, f32, [&](auto lanes, auto wide, auto eight, auto) {
     constexpr int kPer = 8 * decltype(lanes)::value * decltype(eight)::value;
     if (decltype(wide)::value) {
       r.waves = (cols + kPer - 1) / kPer;
@@ -393,9 +402,9 @@ Held held(int cols) {
 // gradients of 54613 x 768 bf16 73.6 us as rows of runs in part, 57.6 so.
 template <bool kBackward, class Launch>
 void by_fill(const Held& h, int cols, bool f32, Launch&& launch) {
-  if (h.exact) by_width<kBackward, kAll>(cols, launch);
-  else if (cols % (f32 ? 4 : 8) == 0) by_width<kBackward, kWhole>(cols, launch);
-  else by_width<kBackward, kPart>(cols, launch);
+  if (h.exact) by_width<kBackward, kAll>(cols, f32, launch);
+  else if (cols % (f32 ? 4 : 8) == 0) by_width<kBackward, kWhole>(cols, f32, launch);
+  else by_width<kBackward, kPart>(cols, f32, launch);
 }
 
 }  // namespace
@@ -404,14 +413,14 @@ void by_fill(const Held& h, int cols, bool f32, Launch&& launch) {
 // four to a CU at most and with no more than 8 MB of sums.  us with one and with four to a CU: 4096 x
 // 1024 fp32 15.8 and 20.3, 16384 x 1024 bf16 25.7 and 29.1; 65536 x 512 fp32 73.1 and 70.7, 100000 x 128
 // fp32 33.2 and 32.1.
-int layer_norm_parts(int64_t rows, int cols) {
-  const Held h = held<true>(cols);
+int layer_norm_parts(int64_t rows, int cols, bool f32) {
+  const Held h = held<true>(cols, f32);
   const int64_t most = h.waves > 1 ? 256 : std::min<int64_t>(rows / 64, std::min(1024, (1 << 20) / cols));
   return int(std::min<int64_t>((rows + h.rows - 1) / h.rows, std::max<int64_t>(256, most)));
 }
 
 hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s) {
-  const Held h = held<false>(a.cols);
+  const Held h = held<false>(a.cols, f32);
   a.waves = h.waves;
   const int64_t turns = (a.rows + h.rows - 1) / h.rows;
   // 8192 x 5120 bf16, us, through and past the caches: 39.9 and 34.2 (where they could hold them, what
@@ -442,9 +451,9 @@ hipError_t launch_layer_norm(LayerNorm a, bool f32, hipStream_t s) {
 }
 
 hipError_t launch_layer_norm_backward(LayerNormBackward a, bool f32, hipStream_t s) {
-  const Held h = held<true>(a.cols);
+  const Held h = held<true>(a.cols, f32);
   a.waves = h.waves;
-  a.num_parts = layer_norm_parts(a.rows, a.cols);
+  a.num_parts = layer_norm_parts(a.rows, a.cols, f32);
   auto launch = [&](auto lanes, auto wide, auto eight, auto fill) {
     constexpr bool kWide = decltype(wide)::value;
     const dim3 block(kWide ? 64 * h.waves * h.rows : kThreads), grid{unsigned(a.num_parts)};
@@ -453,8 +462,9 @@ hipError_t launch_layer_norm_backward(LayerNormBackward a, bool f32, hipStream_t
                                              decltype(eight)::value, decltype(fill)::value>>),
                          grid, block, 0, s, a);
     };
-    if (f32) of(std::true_type{});
-    else of(std::false_type{});
+    if constexpr (!kWide || decltype(eight)::value != 2)
+      if (f32) return of(std::true_type{});
+    of(std::false_type{});
   };
   if (a.rows > 0) {
     by_fill<true>(h, a.cols, f32, launch);

@@ -74,7 +74,7 @@ SHAPES = [(1, 1, 0, 0), (5, 2, 1, 0), (3, 7, 0, 0), (9, 8, 3, 5), (33, 63, 0, 0)
           (1500, 40, 0, 0), (2700, 520, 0, 0), (600, 2056, 0, 8),
           # whole runs that do not fill their lanes, by four and by eight values
           (33, 104, 0, 0), (17, 204, 0, 4), (9, 392, 8, 0), (5, 1540, 0, 0), (1300, 2044, 4, 0),
-          (3, 4456, 0, 0), (2, 11008, 0, 0), (700, 12300, 0, 1)]
+          (3, 4456, 0, 0), (2, 11008, 0, 0), (700, 12300, 0, 1), (1603, 5120, 0, 0)]
 
 
 def data(rows, cols, seed, dtype, wtype):
