@@ -13,7 +13,7 @@ import torch
 
 from . import torch_ops as ops
 from .binding import GNMR_BUDGET_ACTIVE, Controller, gnmr_grouped_wgrad_num_partials
-from .torch_units import clip_from_controller, clippable
+from .torch_units import clip_from_controller, clippable, torch_stream
 
 
 def _readable(dy):
@@ -209,7 +209,7 @@ class ExpertUnits:
                       for n, w in zip(self.names, self.weights)}
         self._filled = [False] * len(self.weights)
         self._started = [0] * len(self.weights)     # gradients started, by matrix
-        self._writers = [None] * len(self.weights)  # the stream that last wrote each
+        self._writers = [None] * len(self.weights)  # the stream that last wrote each, or its handle
         self._replayed = [False] * len(self.weights)    # written by a graph, unseen by the host
         U = first[-1]
         off = np.zeros(U + 1, np.int64)
@@ -276,8 +276,7 @@ class ExpertUnits:
         stream under capture waits only for others of its capture, which end with it."""
         for w in {_handle(w): w for w in writers if w is not None}.values():
             if _handle(w) != _handle(stream):
-                if not hasattr(stream, "wait_stream"):
-                    stream = torch.cuda.ExternalStream(_handle(stream), device=self.device)
+                stream, w = (torch_stream(t, self.device) for t in (stream, w))
                 if _captured(stream) == _captured(w):
                     stream.wait_stream(w)
 
@@ -311,10 +310,12 @@ class ExpertUnits:
         """step(), and then the gradients, with `others` (more gradient tensors of the step), scaled in
         place to a global norm of at most max_norm.  The units' norms are those that the step has just
         made; only `others`, ready on `stream`, are read for the norm.  Returns it (a float64 scalar on the
-        device).  A call that is refused for `others` has not stepped."""
+        device).  A call that is refused for `others` has not stepped.  What takes the gradients here next,
+        an update or the next backward, waits for `stream`."""
         stream, gradients = self._stream(stream), list(self.grads.values())
         others = clippable(gradients, others, max_norm, eps, self.device)
         self.step(alpha_t, beta_t, stream)
+        self._writers = [stream] * len(self.weights)
         return clip_from_controller(self.ctl, gradients, others, max_norm, eps, stream, self.device)
 
     def query(self, stream=None) -> dict:

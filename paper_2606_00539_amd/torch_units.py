@@ -31,6 +31,15 @@ def _current(stream):
     return torch.cuda.current_stream()
 
 
+def torch_stream(stream, device):
+    """`stream` as a stream of torch's; it may be a raw handle of the device's."""
+    import torch
+
+    if hasattr(stream, "wait_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
+
+
 class _DeviceNorms:
     """A controller's norms as an array of device float64; it keeps the controller."""
 
@@ -67,10 +76,7 @@ def clip_from_controller(ctl, gradients, others, max_norm, eps, stream, device):
 
     from .torch_ops import clip_gradients
 
-    if not hasattr(stream, "wait_stream"):
-        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)),
-                                           device=device)
-    with torch.cuda.stream(stream):
+    with torch.cuda.stream(torch_stream(stream, device)):
         norms = torch.as_tensor(_DeviceNorms(ctl), device=device)
         return clip_gradients(gradients + others, max_norm, known=range(len(gradients)),
                               norms=norms, eps=eps)
