@@ -32,12 +32,16 @@ def _current(stream):
 
 
 def torch_stream(stream, device):
-    """`stream` as a stream of torch's; it may be a raw handle of the device's."""
+    """`stream` as a stream of torch's; it may be a raw handle of the device's.  (Of handle 0, the
+    default stream, ExternalStream makes a new one.)"""
     import torch
 
     if hasattr(stream, "wait_stream"):
         return stream
-    return torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
+    handle = int(getattr(stream, "cuda_stream", stream))
+    if handle == 0:
+        return torch.cuda.default_stream(device)
+    return torch.cuda.ExternalStream(handle, device=device)
 
 
 class _DeviceNorms:

@@ -101,3 +101,37 @@ def test_one_stream_waits_for_nothing(machine):
         machine.units.step_clipped(1.1, 1.5, 1.0)
         machine.opt.step()
     assert not any("waits for" in e for e in machine.log)
+
+
+def test_handle_0_is_the_default_stream(machine):
+    """step and step_clipped of the default stream's handle run there, and wait there."""
+    machine.backward(1)
+    machine.units.step_clipped(1.1, 1.5, 1.0, stream=0)
+    assert machine.log[2:] == [(0, "waits for", 1), (0, "steps"), (0, "clips")]
+    machine.backward(5)
+    del machine.log[:]
+    machine.units.step(1.1, 1.5, stream=0)
+    assert machine.log == [(0, "waits for", 5), (0, "steps")]
+
+
+@pytest.mark.parametrize("kind", ["TorchUnits", "FusedWgradUnits"])
+def test_other_units_clip_where_they_step(machine, kind):
+    units = object.__new__(getattr(torch_units, kind))
+    m = torch.nn.Linear(4, 3)
+    m.weight.grad = torch.ones(3, 4)
+    units.modules, units.params, units.param_names = [m], [m.weight], ["w"]
+    units.unit_names, units._produced, units.partials = ["w"], [m.weight.grad.data_ptr()], None
+    on = []
+
+    class Steps:
+        def step(self, alpha, beta, seg_ptr, stream):
+            on.append(int(getattr(stream, "cuda_stream", stream)))
+
+        def step_from_partials(self, partials, alpha, beta, stream):
+            on.append(int(getattr(stream, "cuda_stream", stream)))
+    units.ctl = Steps()
+    for k, given in enumerate((None, 0, 7, Stream(9, machine.log))):
+        units._produced = [m.weight.grad.data_ptr()]
+        units.step_clipped(1.1, 1.5, 1.0, stream=given)
+        assert machine.log[-1] == (on[k], "clips")
+    assert on == [1, 0, 7, 9]

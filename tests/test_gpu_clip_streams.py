@@ -48,3 +48,16 @@ def test_an_update_and_the_next_backward_follow_a_clipping_elsewhere():
     for how in (side, side.cuda_stream):
         got = run(lambda: how)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), how
+
+
+def test_a_handle_of_the_default_stream():
+    """0, also where torch's current stream is another."""
+    torch = require_gpu()
+    want = run(lambda: None)
+    assert torch.cuda.default_stream().cuda_stream == 0
+    side = torch.cuda.Stream()
+    for current in (torch.cuda.default_stream(), side):
+        with torch.cuda.stream(current):
+            got = run(lambda: 0)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
