@@ -210,6 +210,7 @@ class ExpertUnits:
         self._filled = [False] * len(self.weights)
         self._started = [0] * len(self.weights)     # gradients started, by matrix
         self._writers = [None] * len(self.weights)  # the stream that last wrote each, or its handle
+        self._stepped = None                        # the stream of the last step: it reads the sums
         self._replayed = [False] * len(self.weights)    # written by a graph, unseen by the host
         U = first[-1]
         off = np.zeros(U + 1, np.int64)
@@ -271,9 +272,10 @@ class ExpertUnits:
                                         keep)
 
     def _after_writers(self, stream, writers):
-        """Work that follows on `stream` runs after the gradients' writers.  (Backward runs where
-        forward did, on several streams perhaps; autograd orders only what passes through it.)  A
-        stream under capture waits only for others of its capture, which end with it."""
+        """Work that follows on `stream` runs after the gradients' writers, or what reads them.
+        (Backward runs where forward did, on several streams perhaps; autograd orders only what passes
+        through it.)  A stream under capture waits only for others of its capture, which end with
+        it."""
         for w in {_handle(w): w for w in writers if w is not None}.values():
             if _handle(w) != _handle(stream):
                 stream, w = (torch_stream(t, self.device) for t in (stream, w))
@@ -282,7 +284,8 @@ class ExpertUnits:
 
     def _weight_grad(self, k, dy, x, offsets):
         E, stream = self.weights[k].shape[0], self._stream(None)
-        self._after_writers(stream, self._writers[k:k + 1])
+        # (what follows a gradient's start is behind the step with that)
+        self._after_writers(stream, [self._writers[k], None if self._filled[k] else self._stepped])
         ops.grouped_wgrad(dy, x, offsets, dw=self.grads[self.names[k]],
                           accumulate=self._filled[k],
                           partials=self.partials[self._parts[k]:self._parts[k + 1]].view(E, -1))
@@ -303,6 +306,7 @@ class ExpertUnits:
         stream = self._stream(stream)
         self._after_writers(stream, self._writers)
         self.ctl.step_from_partials(self.partials, alpha_t, beta_t, stream)
+        self._stepped = stream
         self._filled = [False] * len(self.weights)
 
     def step_clipped(self, alpha_t: float, beta_t: float, max_norm: float, others=(),

@@ -1,5 +1,5 @@
-"""Where step_clipped runs, and what waits for it, on the CPU with streams that only note what
-waits for what."""
+"""Where steps and step_clipped run, and what waits for them, on the CPU with streams that only
+note what waits for what."""
 import contextlib
 
 import pytest
@@ -93,6 +93,23 @@ def test_the_next_gradients_wait_for_the_clipping(machine, how):
     assert machine.log == [(5, "waits for", 7), (5, "writes")] * 2
     machine.units.step_clipped(1.1, 1.5, 1.0, stream=machine.streams(7)[how])
     assert machine.log[4:] == [(7, "waits for", 5), (7, "steps"), (7, "clips")]
+
+
+@pytest.mark.parametrize("how", [0, 1])
+def test_the_next_sums_of_squares_wait_for_the_step(machine, how):
+    """The controller reads those of the last gradients, where the next ones go."""
+    machine.backward(1)
+    machine.units.step(1.1, 1.5, stream=machine.streams(7)[how])
+    del machine.log[:]
+    machine.backward(1)
+    assert machine.log == [(1, "waits for", 7), (1, "writes")] * 2
+    del machine.log[:]
+    machine.backward(1)                 # another micro-batch, behind the first
+    assert machine.log == [(1, "writes")] * 2
+    machine.units.step(1.1, 1.5)
+    del machine.log[:]
+    machine.backward(1)
+    assert machine.log == [(1, "writes")] * 2
 
 
 def test_one_stream_waits_for_nothing(machine):

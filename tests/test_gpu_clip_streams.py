@@ -61,3 +61,33 @@ def test_a_handle_of_the_default_stream():
             got = run(lambda: 0)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_step_elsewhere_reads_its_own_gradients_sums():
+    """A late controller step on another stream, and the next backward at once."""
+    torch = require_gpu()
+    from paper_2606_00539_amd.torch_experts import ExpertUnits
+
+    g = torch.Generator(device="cuda").manual_seed(22)
+    w = torch.nn.Parameter((torch.randn(4, 136, 128, generator=g, device="cuda") / 11).bfloat16())
+    off = torch.tensor([0, 10, 11, 40, 64], dtype=torch.int32, device="cuda")
+    x = [torch.randn(64, 128, generator=g, device="cuda").bfloat16() * 2.0 ** k for k in range(4)]
+    side = torch.cuda.Stream()
+
+    def last_norms(given, n):
+        """The norms of step n, with a backward behind it."""
+        units = ExpertUnits([("m", w)], max_o=2, lock_len=1, low_cost=False)
+        torch.cuda.synchronize()
+        for v in x[:n]:
+            units.linear("m", v, off).float().square().sum().backward()
+            with torch.cuda.stream(given):
+                torch.cuda._sleep(20_000_000)
+            units.step(1.1, 1.5, stream=given)
+        units.linear("m", x[n], off).float().square().sum().backward()
+        out = units.query(stream=given)["norm"]
+        torch.cuda.synchronize()
+        units.close()
+        return out
+    here = torch.cuda.current_stream()
+    for n in (1, 2, 3):
+        assert (last_norms(side, n) == last_norms(here, n)).all()
