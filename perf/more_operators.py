@@ -326,7 +326,11 @@ def _plain_clip(s):
     squares = [g.double().square().sum() for k, g in enumerate(grads) if k not in known]
     norm = torch.sqrt(torch.stack(squares).sum() + s["norms"].square().sum())
     c = torch.clamp(s["max_norm"] / (norm + CLIP_EPS), max=1.0).float()
-    torch._foreach_copy_(outs, [g.float() * c for g in grads])
+    scaled = [g.float() * c for g in grads]
+    # (one type of destinations to a call: one with fp32 ones first and bf16 ones behind has faulted)
+    for t in dict.fromkeys(o.dtype for o in outs):
+        at = [k for k, o in enumerate(outs) if o.dtype == t]
+        torch._foreach_copy_([outs[k] for k in at], [scaled[k] for k in at])
     return {"norm": norm, **s["flat"]}
 
 
