@@ -557,7 +557,8 @@ gnmr_status gnmr_layer_norm_backward(const void* dy, int64_t dy_stride, const vo
  *   c = max_norm / (n + eps) where n + eps > max_norm, else 1 (NaN where n is NaN);  out = c in
  * norms: device double [num_norms] of what is known (the controller's norms of
  * gnmr_device_outputs, so that gradients that it has stepped from are not read again: set `known`
- * in those).  Sums and products are in float64, in an order that the sizes fix: deterministic.
+ * in those).  Sums and products are in float64, in an order that the sizes fix: deterministic; each
+ * product is rounded once to its out_dtype.
  * norm: device double, gets n.  max_norm >= 0 (infinity: the norm alone), eps >= 0.  Gradients in
  * place with c = 1 are not touched.  gradients: host array, read during the call; outs may overlap
  * nothing but their own `in`, and that only in place.  workspace: device, 16-byte aligned, of
@@ -567,7 +568,7 @@ typedef struct {
   void* out;           /* device; equal to `in` (of one type): in place            */
   int64_t numel;       /* >= 0; 2^44 values in all at most                         */
   int32_t in_dtype;    /* GNMR_F32 or GNMR_BF16                                    */
-  int32_t out_dtype;   /* GNMR_F32 or GNMR_BF16 (rounded once)                     */
+  int32_t out_dtype;   /* GNMR_F32 or GNMR_BF16                                    */
   int32_t known;       /* 1: its squares are in `norms`                            */
   int32_t reserved;
 } gnmr_gradient;
