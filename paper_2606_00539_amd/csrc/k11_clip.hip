@@ -185,7 +185,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
   }
 }
 
-// launch(the tensors, in an argument of 1 KB where they fit one): the host copies it whole.
+// launch(the tensors, in an argument of 1 KB where they fit one): the host copies it whole.  Calls with
+// tensors of 4,096 values, us, medians of three runs in turn with it and with the long one alone: 28 tensors
+// 21.3 and 21.5, 30 21.4 and 21.8, 8 the same.
 template <class Launch>
 void with_few(const ClipTensors& t, Launch&& launch) {
   if (t.num > kClipFew) return launch(t);
