@@ -530,8 +530,9 @@ gnmr_status gnmr_gated_dgrad(const gnmr_groups* groups, const void* dy, int64_t 
  * x, y: device, of x_dtype (GNMR_F32 or GNMR_BF16), rows *_stride elements apart (cols .. 2^28, any
  * parity), aligned to their elements; weight, bias: device [cols] of weight_dtype, or NULL (1 and
  * 0); mean, rstd: device float [rows], what the gradients need, or NULL.  cols 1 .. 16384, rows up
- * to 16,777,215.  Squares of deviations have to stay below 2^128; a row with an infinity or a NaN
- * is NaN. */
+ * to 16,777,215.  In fp32's range have to stay: the sum of a row, the sum of the squares of its
+ * deviations (below 2^128) and, with eps 0, their mean (2^-126 or more).  A row with an infinity or
+ * a NaN is NaN. */
 gnmr_status gnmr_layer_norm(const void* x, int32_t x_dtype, int64_t x_stride, const void* weight,
                             const void* bias, int32_t weight_dtype, void* y, int64_t y_stride,
                             float* mean, float* rstd, int64_t rows, int32_t cols, float eps,
@@ -541,7 +542,8 @@ gnmr_status gnmr_layer_norm(const void* x, int32_t x_dtype, int64_t x_stride, co
  *   g = dy weight, z = (x - mean) rstd;  dx = rstd (g - sum g / cols - z sum(g z) / cols),
  *   dweight = sum over rows of dy z,  dbias = sum over rows of dy
  * dx of x's type, dweight and dbias [cols] of weight_dtype; each may be NULL (not wanted).  The sums over
- * rows are fp32, in an order that rows and cols fix: deterministic.  No rows give dweight and dbias 0.
+ * rows are fp32, in an order that rows and cols fix: deterministic.  A row's sums of g and of
+ * g (x - mean) have to stay below 2^128.  No rows give dweight and dbias 0.
  * workspace: device, 16-byte aligned, of at least gnmr_layer_norm_backward_workspace(rows, cols)
  * bytes; NULL where neither dweight nor dbias is wanted. */
 int64_t gnmr_layer_norm_backward_workspace(int64_t rows, int32_t cols);
@@ -557,7 +559,7 @@ gnmr_status gnmr_layer_norm_backward(const void* dy, int64_t dy_stride, const vo
  *   c = max_norm / (n + eps) where n + eps > max_norm, else 1 (NaN where n is NaN);  out = c in
  * norms: device double [num_norms] of what is known (the controller's norms of
  * gnmr_device_outputs, so that gradients that it has stepped from are not read again: set `known`
- * in those).  Sums and products are in float64, in an order that the sizes fix: deterministic; each
+ * in those; they are roots of fp32 sums, infinite from 2^64 on).  Sums and products are in float64, in an order that the sizes fix: deterministic; each
  * product is rounded once to its out_dtype.
  * norm: device double, gets n.  max_norm >= 0 (infinity: the norm alone), eps >= 0.  Gradients in
  * place with c = 1 are not touched.  gradients: host array, read during the call; outs may overlap

@@ -75,7 +75,10 @@ def clippable(gradients, others, max_norm, eps, device):
 def clip_from_controller(ctl, gradients, others, max_norm, eps, stream, device):
     """The gradients that ctl has just stepped from, which are all of its units', and `others`
     scaled in place to a global norm of at most max_norm, on `stream`; returns the norm.  Only
-    `others` are read for it."""
+    `others` are read for it.  The units' norms are the controller's, roots of fp32 sums of squares:
+    one of 2^64 or more is infinite, and then so is the global norm, and everything is scaled by 0, as
+    with an infinity among the gradients; of values below 2^-63 few digits count, and none of those below
+    2^-75."""
     import torch
 
     from .torch_ops import clip_gradients
@@ -145,8 +148,9 @@ class TorchUnits:
         """step(), and then the units' gradients, with `others` (gradients of parameters that are no
         unit's), scaled in place to a global norm of at most max_norm.  The units' norms are those that
         the step has just made, so their gradients are read once less than by a norm of their own.
-        Returns the norm (a float64 scalar on the device).  `others` are ready on `stream`, as the units'
-        gradients are; a call that is refused for them has not stepped."""
+        Returns the norm (a float64 scalar on the device).  A unit's norm of 2^64 or more is infinite, and
+        then everything is scaled by 0; values below 2^-75 do not count in it.  `others` are ready on
+        `stream`, as the units' gradients are; a call that is refused for them has not stepped."""
         stream, device = _current(stream), self.params[0].device
         gradients = [p.grad for p in self.params]
         others = clippable(gradients, others, max_norm, eps, device)
@@ -346,7 +350,8 @@ class FusedWgradUnits:
         """step(), and then the weights' gradients, with `others` (the biases', for instance), scaled in
         place to a global norm of at most max_norm.  The weights' norms are those that the step has
         just made: their gradients are not read for it.  Returns the norm (a float64 scalar on the
-        device)."""
+        device).  A unit's norm of 2^64 or more is infinite, and then everything is scaled by 0; values
+        below 2^-75 do not count in it."""
         stream, device = _current(stream), self.modules[0].weight.device
         gradients = [m.weight.grad for m in self.modules]
         others = clippable(gradients, others, max_norm, eps, device)
