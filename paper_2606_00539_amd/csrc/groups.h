@@ -235,14 +235,15 @@ inline int grouped_tile(const GroupArgs& g, int N, int K, int weight, double bes
 
 // Tiles of products one after the other on a CU (mm_stream.h), and whether that is the way for a
 // product of grouped rows, `bytes` of memory to each value of whose result are read and written at its
-// tiles' ends.  A call takes 4 us, a step 0.70 and the bytes of a tile's end 64 KB to a us: fitted to 65
-// shapes (300 to 65,536 rows, up to 128 groups, K 256 to 4096), for 15 of whose 195 calls the slower way is
-// taken by 5 to 10%, for the others by less or not at all.  us one after the other, and in tiles of the
-// best edge: 24,640 rows in 64 groups, 2048 to 2 x 1408, both products and h (3 bytes) 344 and 423, h alone
-// (1) 320 and 344, the gradient (8) 222 and 235; 5,000 rows in 64 groups, 4096 to 2 x 2752, 573 and 749;
-// 9,000 rows in 8 groups, 320 to 2 x 688, 20.8 and 24.8; 8,192 rows, 4096 to 2 x 11008, 1,151 and 1,103.
+// tiles' ends.  A call takes 4 us, a step `step` and the bytes of a tile's end 64 KB to a us.  With the
+// products and for the gradient fitted to 65 shapes (300 to 65,536 rows, up to 128 groups, K 256 to 4096): for
+// 5 of their 130 calls the slower way is taken by 5 to 10%, for the others by less or not at all.  us one after
+// the other, and in tiles of the best edge: 24,640 rows in 64 groups, 2048 to 2 x 1408, both products and h
+// (3 bytes) 344 and 423, the gradient (8) 222 and 235; 5,000 rows in 64 groups, 4096 to 2 x 2752, 573 and 749;
+// 9,000 rows in 8 groups, 320 to 2 x 688, 20.8 and 24.8; but 8,192 rows, 4096 to 2 x 11008, 1,151 and 1,103,
+// 5120 to 2 x 13824, 2,100 and 1,910.
 constexpr int kStreamM = 128, kStreamN = 256;
-inline bool streams(const GroupArgs& g, int N, int K, double beside, double bytes) {
+inline bool streams(const GroupArgs& g, int N, int K, double beside, double bytes, double step = 0.70) {
   if (K % 64 != 0 || K < 256) return false;     // (whole steps, two rounds of three at least)
   double tiles_us;
   grouped_tile(g, N, K, 2, beside, &tiles_us);
@@ -250,7 +251,7 @@ inline bool streams(const GroupArgs& g, int N, int K, double beside, double byte
   const double tiles = ceil(double(g.rows) / kStreamM + (g.offsets == nullptr ? 0.0 : 0.5 * used)) *
                        ceil(double(N) / kStreamN);
   const double steps = ceil(K / 192.0) * 3.0;
-  return 4.0 + ceil(tiles / 256.0) * (0.70 * steps + kStreamM * kStreamN * bytes / 64e3) < tiles_us;
+  return 4.0 + ceil(tiles / 256.0) * (step * steps + kStreamM * kStreamN * bytes / 64e3) < tiles_us;
 }
 
 // The launches of a batch of products of K8: X X^T and A A, symmetric (tiles on and above the
@@ -324,8 +325,18 @@ inline bool gated_weights_once(const GroupArgs& g) { return g.rows <= 64 * int64
 
 // (Weights that are read once: tiles of 64.  4,096 rows in 64 groups, 2048 to 2 x 1408, us: 163 in them
 // and 176 one after the other; 2,048 rows 156 and 177.)
+//
+// h alone leaves little at a tile's end, so that it gains less from tiles one after the other: there a step
+// counts as 0.78 us, and the tiles' ends as two bytes less than those of a whole product.  Fitted to 143
+// shapes (209 to 65,536 rows, K 256 to 8192): for 4 the slower way is taken by 5 to 10%, for one by 17%; 0.6%
+// is lost on average (1.9% counted as the others, 2.9% in tiles alone).  us one after the other, and in tiles:
+// 8,192 rows, 4096 to 2 x 11008, 1,161 and 1,086; 5120 to 2 x 13824, 2,008 and 1,791; 32,768 rows in 16 groups,
+// 2048 to 2 x 1408, 351 and 334, but 24,640 rows in 64 groups 320 and 344.
+constexpr double kAloneStep = 0.78, kAloneBeside = -2.0, kAloneBytes = 2.0;
 inline bool gated_linear_streams(const GroupArgs& g, int H, int K, bool keep) {
-  return !gated_weights_once(g) && streams(g, 2 * H, K, keep ? 1.0 : 0.0, keep ? 3.0 : 1.0);
+  if (gated_weights_once(g)) return false;
+  return keep ? streams(g, 2 * H, K, 1.0, 3.0)
+              : streams(g, 2 * H, K, kAloneBeside, kAloneBytes, kAloneStep);
 }
 
 // Makes them: launch(edge, share, workgroups), with *tiles_n set.
