@@ -318,9 +318,11 @@ inline bool gated_dgrad_streams(const GroupArgs& g, int H, int K) {
 }
 
 // Whether a gated block's 64 tiles, which then mostly have a group's rows in one, read its weights
-// past the caches.  us through and past the
-// caches: 64 experts 2048 x 1408, 48 rows 85 and 77.5, 1,536 rows 146 and 133; 8 of 4096 x 11008, 64
-// rows 249 and 223 (6.5 TB/s).
+// past the caches.  us through and past the caches, of weights that these do not hold from one call to the
+// next: 64 experts 2048 x 1408, 48 rows 80 and 74, 1,536 rows 169 and 136; 8 of 4096 x 11008, 64 rows 242 and
+// 215; 16 rows of one matrix of several by turns, 2 x 11008 x 4096 41.8 and 39.0, 2 x 13824 x 5120 57.8 and
+// 54.5, 2 x 5504 x 2048 14.5 and 14.2.  The same matrix in every call, as in a model of less than 256 MB in all,
+// would be there yet: 29.9 and 34.9, 48.1 and 52.1, 9.8 and 13.3; a call cannot tell.
 inline bool gated_weights_once(const GroupArgs& g) { return g.rows <= 64 * int64_t(g.num); }
 
 // (Weights that are read once: tiles of 64.  4,096 rows in 64 groups, 2048 to 2 x 1408, us: 163 in them

@@ -12,7 +12,10 @@
 //
 // Bound by the rows' bytes.  42M values, TB/s of forward and gradients: fp32 6.0 to 6.5 and 5.3 to 6.0 at widths
 // from 768 to 11,008 (odd ones 4.8 and 5.5), bf16 3.7 to 4.6 and 3.4 to 4.9 (odd ones 3.4 and 2.4), where the
-// conversions and the gradients' sums take as long as the bytes.
+// conversions, the gradients' sums and the comparisons of incomplete rows take as long as the bytes.
+//
+// Of the gradients' shapes two spill: two whole runs of bf16 six registers, outside of any loop, and fp32 rows
+// of more than 8,192 columns in part three, of which a row reads two back.
 #include <algorithm>
 
 #include "gnmr_internal.h"

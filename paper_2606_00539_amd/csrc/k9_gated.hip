@@ -13,9 +13,14 @@
 // kept) nor d goes to memory.
 //
 // Bounds and times: a token's experts' weights for few rows (48 rows in 35 of 64 experts, 2048 to 2 x 1408:
-// 404 MB in 78 us, 5.2 TB/s); the chip's power in 256 tiles for many (8,192 rows, 4096 to 2 x 11008: 1,106
-// us, 1,340 TFLOP/s); weights from memory and the ends of ragged groups between them (24,576 rows in 64
-// experts, 2048 to 2 x 1408 with p: 343 us, 830 TFLOP/s; its gradient 215 us).
+// 404 MB in 78 us, 5.2 TB/s); the chip's power in 256 tiles for many (8,192 rows, 4096 to 2 x 11008: 1,112
+// us, 1,330 TFLOP/s; with p 1,160 to 1,240 one after the other); weights from memory and the ends of ragged
+// groups between them (24,576 rows in 64 experts, 2048 to 2 x 1408 with p: 341 to 360 us on several cards, 790
+// to 830 TFLOP/s; its gradient 218 to 228 us).  h from 8,192 x 2 x 11008 products that are there takes
+// 113 us, 4.8 TB/s.
+//
+// 256 tiles with p spill 17 registers (silu) or 18 at the end of their products, outside of any loop, those
+// of h alone one.
 #include <type_traits>
 
 #include "gnmr_internal.h"
