@@ -353,7 +353,8 @@ def _vectors(x, cols, **vectors):
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
     """(y, mean, rstd): layer norm over x's last dimension, y = (x - mean) rstd weight + bias, and
     the fp32 statistics of each row that layer_norm_backward takes.  x: bf16 or fp32, any leading
-    dimensions and row strides; weight and bias: bf16 or fp32, of one type, or None."""
+    dimensions and row strides, 1 to 16384 columns and up to 16,777,215 rows; weight and bias: bf16 or
+    fp32, of one type, or None."""
     kind = _DTYPES.get(x.dtype)
     if kind is None or not x.is_cuda or x.dim() < 1:
         raise TypeError("x must be a bf16 or fp32 tensor of rows on a HIP device")
