@@ -299,7 +299,8 @@ class ExpertUnits:
         self._filled = [False] * len(self.weights)
 
     def step(self, alpha_t: float, beta_t: float, stream=None) -> None:
-        """One controller step from the gradients since the last one (asynchronous)."""
+        """One controller step from the gradients since the last one (asynchronous).  The next
+        gradients wait for `stream`, which lives until then."""
         for n, done in zip(self.names, self._filled):
             if not done:
                 raise RuntimeError(f"{n}: no gradient was written since the last step")

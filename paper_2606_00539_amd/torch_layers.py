@@ -32,8 +32,8 @@ class _LayerNorm(torch.autograd.Function):
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """Layer norm over x's last dimension (K10), with the gradients of x, weight and bias.  x: bf16
     or fp32 on a HIP device, 1 to 16384 columns, up to 16,777,215 rows; weight and bias: bf16 or fp32,
-    both of one type.  Second derivatives are refused.  As with torch's own operators, backward is captured in a graph
-    only while no autograd graph made outside the capture holds the same leaves."""
+    both of one type.  Second derivatives are refused.  As with torch's own operators, backward is
+    captured in a graph only while no autograd graph made outside the capture holds the same leaves."""
     return _LayerNorm.apply(x, weight, bias, eps)
 
 
