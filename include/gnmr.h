@@ -559,8 +559,8 @@ gnmr_status gnmr_layer_norm_backward(const void* dy, int64_t dy_stride, const vo
  *   c = max_norm / (n + eps) where n + eps > max_norm, else 1 (NaN where n is NaN);  out = c in
  * norms: device double [num_norms] of what is known (the controller's norms of
  * gnmr_device_outputs, so that gradients that it has stepped from are not read again: set `known`
- * in those; they are roots of fp32 sums, infinite from 2^64 on).  Sums and products are in float64, in an order that the sizes fix: deterministic; each
- * product is rounded once to its out_dtype.
+ * in those; they are roots of fp32 sums, infinite from 2^64 on).  Sums and products are in float64,
+ * in an order that the sizes fix: deterministic; each product is rounded once to its out_dtype.
  * norm: device double, gets n.  max_norm >= 0 (infinity: the norm alone), eps >= 0.  Gradients in
  * place with c = 1 are not touched.  gradients: host array, read during the call; outs may overlap
  * nothing but their own `in`, and that only in place.  workspace: device, 16-byte aligned, of

@@ -315,9 +315,9 @@ class ExpertUnits:
         """step(), and then the gradients, with `others` (more gradient tensors of the step), scaled in
         place to a global norm of at most max_norm.  The units' norms are those that the step has just
         made; only `others`, ready on `stream`, are read for the norm.  Returns it (a float64 scalar on the
-        device, there on `stream`).  A unit's norm of 2^64 or more is infinite, and then everything is scaled by 0; values
-        below 2^-75 do not count in it.  A call that is refused for `others` has not stepped.  What takes the gradients here next,
-        an update or the next backward, waits for `stream`."""
+        device, there on `stream`).  A unit's norm of 2^64 or more is infinite, and then everything is
+        scaled by 0; values below 2^-75 do not count in it.  A call that is refused for `others` has not
+        stepped.  What takes the gradients here next, an update or the next backward, waits for `stream`."""
         stream, gradients = self._stream(stream), list(self.grads.values())
         others = clippable(gradients, others, max_norm, eps, self.device)
         self.step(alpha_t, beta_t, stream)

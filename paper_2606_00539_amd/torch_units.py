@@ -148,9 +148,10 @@ class TorchUnits:
         """step(), and then the units' gradients, with `others` (gradients of parameters that are no
         unit's), scaled in place to a global norm of at most max_norm.  The units' norms are those that
         the step has just made, so their gradients are read once less than by a norm of their own.
-        Returns the norm (a float64 scalar on the device, there on `stream`).  A unit's norm of 2^64 or more is infinite, and
-        then everything is scaled by 0; values below 2^-75 do not count in it.  `others` are ready on
-        `stream`, as the units' gradients are; a call that is refused for them has not stepped."""
+        Returns the norm (a float64 scalar on the device, there on `stream`).  A unit's norm of 2^64 or
+        more is infinite, and then everything is scaled by 0; values below 2^-75 do not count in it.
+        `others` are ready on `stream`, as the units' gradients are; a call that is refused for them has
+        not stepped."""
         stream, device = _current(stream), self.params[0].device
         gradients = [p.grad for p in self.params]
         others = clippable(gradients, others, max_norm, eps, device)
